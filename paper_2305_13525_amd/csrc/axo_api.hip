@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "axo_common.hpp"
+#include "axo_host.hpp"
 #include "bias_grad.hpp"
 #include "gemm_generic.hpp"
 #include "gemm_group.hpp"
@@ -30,54 +31,11 @@
 constexpr size_t STATIC_SCRATCH_BYTES = 256 * 1024;
 static __device__ __align__(256) unsigned char scratch[STATIC_SCRATCH_BYTES];
 
+using namespace axo_host;
+
 namespace {
 
 using axo::GemmArgs;
-
-struct Shard {
-    int64_t M, Kl, Nl, row0, k0, n0;
-    int k_coord;  // coordinate along the axis that splits K
-};
-
-int derive_shard(const axo_problem_t* p, Shard* s) {
-    if (!p) return AXO_ERR_NULL_PTR;
-    if (p->reserved != 0 || (p->transposed != 0 && p->transposed != 1)) return AXO_ERR_BAD_ARG;
-    if (p->Gx < 1 || p->Gy < 1 || p->Gz < 1) return AXO_ERR_BAD_GRID;
-    if (p->ix < 0 || p->ix >= p->Gx || p->iy < 0 || p->iy >= p->Gy || p->iz < 0 || p->iz >= p->Gz)
-        return AXO_ERR_BAD_COORD;
-    if (p->T < 0 || p->K < 0 || p->N < 0) return AXO_ERR_BAD_SIZE;
-    // Section 3.2: I is cut over the token axis (Z) and the reduction axis, W over the reduction
-    // axis and the output axis.  transposed swaps which of X / Y plays which role.
-    const int gk = p->transposed ? p->Gy : p->Gx, ik = p->transposed ? p->iy : p->ix;
-    const int gn = p->transposed ? p->Gx : p->Gy, in = p->transposed ? p->ix : p->iy;
-    if (p->T % p->Gz != 0 || p->K % gk != 0 || p->N % gn != 0) return AXO_ERR_INDIVISIBLE;
-    s->M = p->T / p->Gz;
-    s->Kl = p->K / gk;
-    s->Nl = p->N / gn;
-    if (s->M > INT32_MAX || s->Kl > INT32_MAX || s->Nl > INT32_MAX) return AXO_ERR_BAD_SIZE;
-    s->row0 = s->M * p->iz;
-    s->k0 = s->Kl * ik;
-    s->n0 = s->Nl * in;
-    s->k_coord = ik;
-    return AXO_OK;
-}
-
-bool aligned16(const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0; }
-
-// One matrix argument: pointer, leading dimension, row length.  A matrix without elements is
-// never dereferenced, so nothing about it is checked.
-int check_matrix(const void* ptr, int64_t ld, int64_t rows, int64_t row_len) {
-    if (rows == 0 || row_len == 0) return AXO_OK;
-    if (!ptr) return AXO_ERR_NULL_PTR;
-    if (ld < row_len) return AXO_ERR_BAD_LD;
-    if (!aligned16(ptr) || (ld % 8) != 0) return AXO_ERR_MISALIGNED;
-    return AXO_OK;
-}
-
-// A launch's threads per grid dimension have to stay below 2^32.  Thin outputs of hundreds of millions of rows or
-// columns pass that with the smaller tiles; the choices below then fall through to a kernel that takes them.
-bool grid_fits(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
-int64_t tiles_in(int n, int size) { return ((int64_t)n + size - 1) / size; }
 
 int launch_generic(const GemmArgs& g, int la, int lb, hipStream_t st) {
     dim3 grid((g.No + axo::GEN_BN - 1) / axo::GEN_BN, (g.Mo + axo::GEN_BM - 1) / axo::GEN_BM, 1);
@@ -92,10 +50,6 @@ int launch_generic(const GemmArgs& g, int la, int lb, hipStream_t st) {
     return hipGetLastError() == hipSuccess ? AXO_OK : AXO_ERR_HIP;
 }
 
-// The tuned kernel covers the output with 256x256 tiles and, to balance tile counts that do not
-// fill the last round of CUs, a region of 256x128 tiles.  The CU count is a design constant
-// (MI355X: 256 CUs) so that planning needs no device.
-constexpr int NUM_CU = 256;
 // relative cost of a half-width tile (half the flops at lower efficiency: more operand traffic
 // per flop), in units of one big tile; measured on MI355X
 constexpr double SMALL_TILE_COST = 0.60;
@@ -178,23 +132,6 @@ axo::TileSched plan_tiles(int Mo, int No) {
     if (cache.size() < 4096) cache[{sc.tiles_m, halves}] = sc;
     return sc;
 }
-
-// The tuned kernels' dynamic LDS size is above the default limit, so the limit is raised once per
-// kernel and device (`raised` holds one bit per device ordinal; a process rarely sees more than
-// 8, and beyond 64 the attribute is simply set on every launch).
-bool raise_lds_limit(const void* kernel, int bytes, std::atomic<uint64_t>* raised) {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return false;
-    const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
-    if (bit && (raised->load(std::memory_order_acquire) & bit)) return true;
-    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
-        return false;
-    raised->fetch_or(bit, std::memory_order_release);
-    return true;
-}
-
-int64_t steps_in(int R) { return tiles_in(R, axo::TILE_BK); }
-int64_t rounds_of(int64_t tiles) { return (tiles + NUM_CU - 1) / NUM_CU; }
 
 // Estimated kernel time in microseconds of a product on its own, from its sizes alone.
 // 256-row tiles: half-width tiles where they have a CU each, else large ones, else rounds of either.  A reduction step of a
@@ -1065,40 +1002,6 @@ int plan_chain_ext(const axo_layer_ext_t* layers, int n_layers, void* ws, size_t
 }
 
 // ---- dependence analysis of a chain --------------------------------------------------------
-// Byte range [lo, hi) that a matrix argument covers (rows x row_len elements of elem bytes, rows
-// ld elements apart); empty matrices cover nothing.  The matrix itself is kept beside its range
-// for the exact overlap test.
-struct Range {
-    uintptr_t lo, hi;
-    int64_t pitch, rows, width;  // bytes between rows, row count, bytes per row
-    bool overlaps(const Range& o) const { return lo < o.hi && o.lo < hi; }
-    // Do the two matrices share a byte?  (Ranges that overlap need not: two column blocks of one
-    // buffer interleave.)  Row r of this matrix covers [a, a + width) relative to the other's
-    // base; row q of the other covers [q * pitch, q * pitch + width_o); they meet iff
-    // q * pitch < a + width and q * pitch + width_o > a, an interval of q that is clamped to the
-    // other's rows.  Only called when the ranges overlap, which no well-formed call makes them do.
-    bool shares_bytes_with(const Range& o) const {
-        if (!overlaps(o)) return false;
-        auto floor_div = [](int64_t x, int64_t y) { return x / y - ((x % y != 0) && ((x < 0) != (y < 0)) ? 1 : 0); };
-        const int64_t op = o.rows > 1 ? o.pitch : (int64_t)(o.hi - o.lo) + 1;  // one row: any positive pitch
-        for (int64_t r = 0; r < rows; ++r) {
-            const int64_t a = (int64_t)(lo - o.lo) + r * pitch;
-            const int64_t q_hi = std::min<int64_t>(floor_div(a + width - 1, op), o.rows - 1);
-            const int64_t q_lo = std::max<int64_t>(floor_div(a - o.width, op) + 1, 0);
-            if (q_lo <= q_hi) return true;
-        }
-        return false;
-    }
-};
-bool matrix_range(const void* ptr, int64_t ld, int64_t rows, int64_t row_len, int elem, Range* r) {
-    if (!ptr || rows <= 0 || row_len <= 0) return false;
-    r->lo = reinterpret_cast<uintptr_t>(ptr);
-    r->hi = r->lo + (uintptr_t)(((rows - 1) * ld + row_len) * elem);
-    r->pitch = ld * elem;
-    r->rows = rows;
-    r->width = row_len * elem;
-    return true;
-}
 // What one product reads and writes.  (Ranges, not elements: two column blocks interleaved in one
 // buffer count as overlapping, which only costs concurrency.)
 struct Footprint {
@@ -1362,20 +1265,23 @@ int plan_query(const axo_problem_t* p, int op, int64_t ld_a, int64_t ld_b, int64
     return plan_query(p, op, made_up(1), ld_a, made_up(2), ld_b, made_up(3), ld_out, pl);
 }
 
-// No exception leaves the library: the planners keep their lists and caches in standard
-// containers, whose allocations can fail.
-template <typename F>
-int guarded(F&& body) noexcept {
-    try {
-        return body();
-    } catch (const std::bad_alloc&) {
-        return AXO_ERR_NO_MEMORY;
-    } catch (...) {
-        return AXO_ERR_BAD_ARG;
+}  // namespace
+
+namespace axo_host {
+
+int launch_products(const GemmArgs* products, int n, int la, int lb, hipStream_t st) {
+    std::vector<Plan> plans((size_t)n);
+    for (int i = 0; i < n; ++i) {
+        plans[i].g = products[i];
+        plans[i].la = la;
+        plans[i].lb = lb;
     }
+    return by_level(plans, std::vector<int>((size_t)n, 0), 1, Enqueue{st});
 }
 
-}  // namespace
+axo::TileSched plan_columns(int Mo, int No) { return plan_tiles(Mo, No); }
+
+}  // namespace axo_host
 
 extern "C" {
 
@@ -1614,3 +1520,5 @@ int axo_layer_step_tiles(const axo_layer_ext_t* layers, int n_layers, int* tiles
 }
 
 }  // extern "C"
+
+#include "axo_block.hpp"  // the entry points of include/axo_block.h

@@ -1,0 +1,521 @@
+// Entry points of include/axo_block.h: validation, choice of kernels, launches.  Part of axo_api.hip's translation unit.
+#pragma once
+#include "../../include/axo_block.h"
+
+#include <cmath>
+#include <initializer_list>
+
+#include "axo_host.hpp"
+#include "gated.hpp"
+#include "norm.hpp"
+
+namespace axo_block {
+
+using namespace axo_host;
+using axo::bf16_t;
+using axo::GatedArgs;
+
+inline int launched() { return hipGetLastError() == hipSuccess ? AXO_OK : AXO_ERR_HIP; }
+// Workgroups of a grid whose workgroups walk over rows or chunks until none are left.
+inline unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)std::max<int64_t>(1, std::min(blocks, most)); }
+
+// A call's matrices: what it reads and what it writes.  An output that shares a byte with an input or another output is refused.
+struct Buffers {
+    Range in[6], out[4];
+    int n_in = 0, n_out = 0;
+    void reads(const void* p, int64_t ld, int64_t rows, int64_t cols, int elem) {
+        if (matrix_range(p, ld, rows, cols, elem, &in[n_in])) ++n_in;
+    }
+    void writes(const void* p, int64_t ld, int64_t rows, int64_t cols, int elem) {
+        if (matrix_range(p, ld, rows, cols, elem, &out[n_out])) ++n_out;
+    }
+    int check() const {
+        for (int o = 0; o < n_out; ++o) {
+            for (int i = 0; i < n_in; ++i)
+                if (out[o].shares_bytes_with(in[i])) return AXO_ERR_BAD_ARG;
+            for (int q = 0; q < o; ++q)
+                if (out[o].shares_bytes_with(out[q])) return AXO_ERR_BAD_ARG;
+        }
+        return AXO_OK;
+    }
+};
+
+// A vector argument: n elements, aligned to `align` bytes; NULL where it is optional.
+inline int check_vector(const void* p, int64_t n, uintptr_t align, bool optional) {
+    if (n == 0) return AXO_OK;
+    if (!p) return optional ? AXO_OK : AXO_ERR_NULL_PTR;
+    return reinterpret_cast<uintptr_t>(p) % align ? AXO_ERR_MISALIGNED : AXO_OK;
+}
+inline int first_error(std::initializer_list<int> statuses) {
+    for (int rc : statuses)
+        if (rc) return rc;
+    return AXO_OK;
+}
+
+// ---- layer norm ----------------------------------------------------------------------------------
+
+int k_axis(const axo_problem_t* p) { return p->transposed ? p->Gy : p->Gx; }
+int elem_of(int type) { return type == AXO_TYPE_F32 ? 4 : 2; }
+bool known_type(int type) { return type == AXO_TYPE_BF16 || type == AXO_TYPE_F32; }
+bool valid_eps(float eps) { return eps >= 0.0f && std::isfinite(eps); }
+
+// A workgroup to a row; more rows than this are walked.
+constexpr int64_t NORM_MOST_BLOCKS = 1 << 20;
+
+int launch_norm(const axo::NormArgs& g, int type, hipStream_t st) {
+    if (g.M == 0 || g.K == 0) return AXO_OK;
+    const dim3 grid(at_most(g.M, NORM_MOST_BLOCKS)), block(axo::NORM_THREADS);
+    if (type == AXO_TYPE_F32) hipLaunchKernelGGL(axo::norm_long_kernel<float>, grid, block, 0, st, g);
+    else hipLaunchKernelGGL(axo::norm_long_kernel<bf16_t>, grid, block, 0, st, g);
+    return launched();
+}
+
+// Row slices of the column sums.
+struct NormSlices {
+    int slices, rows;
+};
+NormSlices norm_slices(int64_t M) {
+    const int64_t rows = std::max<int64_t>(axo::NORM_COL_ROWS, (M + 255) / 256);
+    return {(int)std::max<int64_t>(1, (M + rows - 1) / rows), (int)rows};
+}
+size_t norm_workspace(int64_t M, int64_t K) { return (size_t)norm_slices(M).slices * 2 * (size_t)K * sizeof(float); }
+
+int launch_norm_bwd(axo::NormBwdArgs g, int type, hipStream_t st) {
+    if (g.K == 0) return AXO_OK;
+    if (g.M > 0) {
+        const dim3 grid(at_most(g.M, NORM_MOST_BLOCKS)), block(axo::NORM_THREADS);
+        if (type == AXO_TYPE_F32) hipLaunchKernelGGL(axo::norm_bwd_long_kernel<float>, grid, block, 0, st, g);
+        else hipLaunchKernelGGL(axo::norm_bwd_long_kernel<bf16_t>, grid, block, 0, st, g);
+        if (const int rc = launched()) return rc;
+    }
+    if (g.phase == axo::NORM_APPLY || (!g.dgamma && !g.dbeta)) return AXO_OK;
+    const NormSlices s = norm_slices(g.M);
+    g.slices = s.slices;
+    g.rows_per_slice = s.rows;
+    const dim3 grid((unsigned)(tiles_in(g.K, axo::NORM_STRIP) * s.slices)), block(axo::NORM_COL_THREADS);
+    if (type == AXO_TYPE_F32) hipLaunchKernelGGL(axo::norm_cols_kernel<float>, grid, block, 0, st, g);
+    else hipLaunchKernelGGL(axo::norm_cols_kernel<bf16_t>, grid, block, 0, st, g);
+    if (const int rc = launched()) return rc;
+    hipLaunchKernelGGL(axo::norm_join_kernel, dim3((unsigned)((2 * (int64_t)g.K + 255) / 256)), dim3(256), 0, st, g);
+    return launched();
+}
+
+int plan_norm(const axo_problem_t* p, const void* X, int64_t ldx, const void* R, int64_t ldr, int type, void* S, int64_t lds, Buffers& b,
+              axo::NormArgs& g) {
+    Shard s;
+    if (const int rc = derive_shard(p, &s)) return rc;
+    if (!known_type(type)) return AXO_ERR_BAD_ARG;
+    if (const int rc = check_matrix(X, ldx, s.M, s.Kl)) return rc;
+    if (R)
+        if (const int rc = first_error({check_matrix(R, ldr, s.M, s.Kl), check_matrix(S, lds, s.M, s.Kl)})) return rc;
+    g.X = X; g.ldx = ldx;
+    g.R = R; g.ldr = ldr;
+    g.S = S; g.lds = lds;
+    g.M = (int)s.M; g.K = (int)s.Kl;
+    b.reads(X, ldx, s.M, s.Kl, elem_of(type));
+    if (R) {
+        b.reads(R, ldr, s.M, s.Kl, elem_of(type));
+        b.writes(S, lds, s.M, s.Kl, elem_of(type));
+    }
+    return AXO_OK;
+}
+int plan_norm_output(const void* gamma, const void* beta, float eps, void* Y, int64_t ldy, float* stats, Buffers& b, axo::NormArgs& g) {
+    if (!valid_eps(eps)) return AXO_ERR_BAD_ARG;
+    const int64_t n = g.M > 0 ? g.K : 0;
+    if (const int rc = first_error({check_matrix(Y, ldy, g.M, g.K), check_vector(gamma, n, 16, true), check_vector(beta, n, 16, true),
+                                    check_vector(stats, g.K > 0 ? g.M : 0, 8, true)}))
+        return rc;
+    g.gamma = static_cast<const bf16_t*>(gamma);
+    g.beta = static_cast<const bf16_t*>(beta);
+    g.eps = eps;
+    g.Y = static_cast<bf16_t*>(Y); g.ldy = ldy;
+    g.stats = reinterpret_cast<float2*>(stats);
+    b.reads(gamma, g.K, 1, g.K, 2);
+    b.reads(beta, g.K, 1, g.K, 2);
+    b.writes(Y, ldy, g.M, g.K, 2);
+    b.writes(stats, 2 * (int64_t)g.M, 1, 2 * (int64_t)g.M, 4);
+    return AXO_OK;
+}
+
+int plan_norm_bwd(const axo_problem_t* p, const void* dY, int64_t lddy, const void* S, int64_t lds, int type, const void* gamma,
+                  const float* stats, Buffers& b, axo::NormBwdArgs& g) {
+    Shard s;
+    if (const int rc = derive_shard(p, &s)) return rc;
+    if (!known_type(type)) return AXO_ERR_BAD_ARG;
+    const bool some = s.M > 0 && s.Kl > 0;
+    if (const int rc = first_error({check_matrix(dY, lddy, s.M, s.Kl), check_matrix(S, lds, s.M, s.Kl), check_vector(gamma, some ? s.Kl : 0, 16, true),
+                                    check_vector(stats, some ? s.M : 0, 8, false)}))
+        return rc;
+    g.dY = static_cast<const bf16_t*>(dY); g.lddy = lddy;
+    g.S = S; g.lds = lds;
+    g.gamma = static_cast<const bf16_t*>(gamma);
+    g.stats = reinterpret_cast<const float2*>(stats);
+    g.M = (int)s.M; g.K = (int)s.Kl;
+    g.per_row = p->K > 0 ? 1.0f / (float)p->K : 0.0f;
+    b.reads(dY, lddy, s.M, s.Kl, 2);
+    b.reads(S, lds, s.M, s.Kl, elem_of(type));
+    b.reads(gamma, s.Kl, 1, s.Kl, 2);
+    b.reads(stats, 2 * s.M, 1, 2 * s.M, 4);
+    return AXO_OK;
+}
+int plan_norm_dx(const void* R, int64_t ldr, int type, void* dX, int64_t lddx, Buffers& b, axo::NormBwdArgs& g) {
+    if (R)
+        if (const int rc = check_matrix(R, ldr, g.M, g.K)) return rc;
+    if (const int rc = check_matrix(dX, lddx, g.M, g.K)) return rc;
+    g.R = R; g.ldr = ldr;
+    g.dX = dX; g.lddx = lddx;
+    if (R) b.reads(R, ldr, g.M, g.K, elem_of(type));
+    b.writes(dX, lddx, g.M, g.K, elem_of(type));
+    return AXO_OK;
+}
+int plan_norm_columns(float* dgamma, float* dbeta, int accumulate, void* ws, size_t ws_bytes, Buffers& b, axo::NormBwdArgs& g) {
+    if (accumulate != 0 && accumulate != 1) return AXO_ERR_BAD_ARG;
+    if (const int rc = first_error({check_vector(dgamma, g.K, 4, true), check_vector(dbeta, g.K, 4, true)})) return rc;
+    g.dgamma = dgamma;
+    g.dbeta = dbeta;
+    g.accumulate = accumulate;
+    b.writes(dgamma, g.K, 1, g.K, 4);
+    b.writes(dbeta, g.K, 1, g.K, 4);
+    if ((!dgamma && !dbeta) || g.K == 0) return AXO_OK;
+    const size_t need = norm_workspace(g.M, g.K);
+    if (need == 0) return AXO_OK;
+    if (!ws || ws_bytes < need) return AXO_ERR_WORKSPACE;
+    if (!aligned16(ws)) return AXO_ERR_MISALIGNED;
+    g.partial = static_cast<float*>(ws);
+    b.writes(ws, (int64_t)(need / 4), 1, (int64_t)(need / 4), 4);
+    return AXO_OK;
+}
+
+// ---- gated block -----------------------------------------------------------------------------------
+
+bool known_gate(int gate) { return gate >= AXO_GATE_SILU && gate <= AXO_GATE_GELU_ERF; }
+
+template <int OP>
+int launch_gated_generic(const GatedArgs& g, hipStream_t st) {
+    const dim3 grid((unsigned)tiles_in(g.No, axo::GEN_BN), (unsigned)tiles_in(g.Mo, axo::GEN_BM));
+    if (grid.y > 65535u) return AXO_ERR_BAD_SIZE;
+    hipLaunchKernelGGL(axo::gated_generic_kernel<OP>, grid, dim3(256), 0, st, g);
+    return launched();
+}
+template <int OP>
+int launch_gated(const GatedArgs& g, hipStream_t st) {
+    if (g.Mo == 0 || g.No == 0) return AXO_OK;
+    return launch_gated_generic<OP>(g, st);
+}
+
+size_t gated_workspace(const Shard&) { return 0; }
+int check_gated_workspace(const Shard& s, const void* ws, size_t ws_bytes, Buffers& b) {
+    const size_t need = gated_workspace(s);
+    if (need == 0) return AXO_OK;
+    if (!ws || ws_bytes < need) return AXO_ERR_WORKSPACE;
+    if (!aligned16(ws)) return AXO_ERR_MISALIGNED;
+    b.writes(ws, (int64_t)need, 1, (int64_t)need, 1);
+    return AXO_OK;
+}
+
+int launch_map(const axo::GatedMapArgs& g, bool back, hipStream_t st) {
+    if (g.M == 0 || g.N == 0) return AXO_OK;
+    const dim3 grid(at_most((tiles_in(g.N, 8) * g.M + axo::GATED_MAP_THREADS - 1) / axo::GATED_MAP_THREADS, 1 << 20)), block(axo::GATED_MAP_THREADS);
+    if (back) hipLaunchKernelGGL(axo::gated_map_kernel<true>, grid, block, 0, st, g);
+    else hipLaunchKernelGGL(axo::gated_map_kernel<false>, grid, block, 0, st, g);
+    return launched();
+}
+
+// Two weight gradients.  T: type of the outputs.
+template <typename T>
+int gated_wgrad(const axo_problem_t* p, const void* X, int64_t ldx, const void* dG, const void* dU, int64_t lddz, T* dWg, T* dWu, int64_t lddw,
+                void* ws, size_t ws_bytes, hipStream_t st) {
+    constexpr bool F32 = sizeof(T) == 4;
+    Shard s;
+    if (const int rc = derive_shard(p, &s)) return rc;
+    if (const int rc = first_error({check_matrix(X, ldx, s.M, s.Kl), check_matrix(dG, lddz, s.M, s.Nl), check_matrix(dU, lddz, s.M, s.Nl)})) return rc;
+    for (const T* w : {dWg, dWu}) {
+        if (s.Kl == 0 || s.Nl == 0) break;
+        if (!w) return AXO_ERR_NULL_PTR;
+        if (lddw < s.Nl) return AXO_ERR_BAD_LD;
+        if (!aligned16(w) || lddw % (F32 ? 4 : 8)) return AXO_ERR_MISALIGNED;
+    }
+    Buffers b;
+    b.reads(X, ldx, s.M, s.Kl, 2);
+    b.reads(dG, lddz, s.M, s.Nl, 2);
+    b.reads(dU, lddz, s.M, s.Nl, 2);
+    b.writes(dWg, lddw, s.Kl, s.Nl, sizeof(T));
+    b.writes(dWu, lddw, s.Kl, s.Nl, sizeof(T));
+    if (const int rc = first_error({check_gated_workspace(s, ws, ws_bytes, b), b.check()})) return rc;
+    axo::GemmArgs g[2]{};
+    for (int i = 0; i < 2; ++i) {
+        g[i].A = static_cast<const bf16_t*>(X); g[i].lda = ldx;
+        g[i].B = static_cast<const bf16_t*>(i ? dU : dG); g[i].ldb = lddz;
+        g[i].C = reinterpret_cast<bf16_t*>(i ? dWu : dWg); g[i].ldc = lddw;
+        g[i].Mo = (int)s.Kl; g[i].No = (int)s.Nl; g[i].R = (int)s.M;
+        g[i].epilogue = F32 ? axo::EPI_ACC_F32 : axo::EPI_NONE;
+    }
+    return launch_products(g, 2, axo::MC, axo::MC, st);
+}
+
+}  // namespace axo_block
+
+extern "C" {
+
+int axo_norm_fwd(const axo_problem_t* p, const void* X, int64_t ldx, const void* R, int64_t ldr, int type, const void* gamma, const void* beta,
+                 float eps, void* S, int64_t lds, void* Y, int64_t ldy, float* stats, void* hip_stream) {
+    using namespace axo_block;
+    axo::NormArgs g{};
+    Buffers b;
+    if (const int rc = plan_norm(p, X, ldx, R, ldr, type, S, lds, b, g)) return rc;
+    if (k_axis(p) != 1) return AXO_ERR_BAD_GRID;
+    if (const int rc = plan_norm_output(gamma, beta, eps, Y, ldy, stats, b, g)) return rc;
+    if (const int rc = b.check()) return rc;
+    g.phase = axo::NORM_WHOLE;
+    return launch_norm(g, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_norm_part(const axo_problem_t* p, const void* X, int64_t ldx, const void* R, int64_t ldr, int type, void* S, int64_t lds, float* part,
+                  void* hip_stream) {
+    using namespace axo_block;
+    axo::NormArgs g{};
+    Buffers b;
+    if (const int rc = plan_norm(p, X, ldx, R, ldr, type, S, lds, b, g)) return rc;
+    if (const int rc = check_vector(part, g.K > 0 ? g.M : 0, 8, false)) return rc;
+    b.writes(part, 2 * (int64_t)g.M, 1, 2 * (int64_t)g.M, 4);
+    if (const int rc = b.check()) return rc;
+    g.part = reinterpret_cast<float2*>(part);
+    g.phase = axo::NORM_PART;
+    return launch_norm(g, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_norm_apply(const axo_problem_t* p, const void* S, int64_t lds, int type, const float* parts, int n_parts, const void* gamma,
+                   const void* beta, float eps, void* Y, int64_t ldy, float* stats, void* hip_stream) {
+    using namespace axo_block;
+    axo::NormArgs g{};
+    Buffers b;
+    if (const int rc = plan_norm(p, S, lds, nullptr, 0, type, nullptr, 0, b, g)) return rc;
+    if (n_parts != k_axis(p)) return AXO_ERR_BAD_ARG;
+    if (const int rc = check_vector(parts, g.K > 0 ? g.M : 0, 8, false)) return rc;
+    if (const int rc = plan_norm_output(gamma, beta, eps, Y, ldy, stats, b, g)) return rc;
+    b.reads(parts, 2 * (int64_t)g.M * n_parts, 1, 2 * (int64_t)g.M * n_parts, 4);
+    if (const int rc = b.check()) return rc;
+    g.parts = reinterpret_cast<const float2*>(parts);
+    g.n_parts = n_parts;
+    g.phase = axo::NORM_APPLY;
+    return launch_norm(g, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_norm_bwd(const axo_problem_t* p, const void* dY, int64_t lddy, const void* S, int64_t lds, const void* R, int64_t ldr, int type,
+                 const void* gamma, const float* stats, void* dX, int64_t lddx, float* dgamma, float* dbeta, int accumulate, void* ws,
+                 size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    axo::NormBwdArgs g{};
+    Buffers b;
+    if (const int rc = plan_norm_bwd(p, dY, lddy, S, lds, type, gamma, stats, b, g)) return rc;
+    if (k_axis(p) != 1) return AXO_ERR_BAD_GRID;
+    if (const int rc = first_error({plan_norm_dx(R, ldr, type, dX, lddx, b, g), plan_norm_columns(dgamma, dbeta, accumulate, ws, ws_bytes, b, g)})) return rc;
+    if (const int rc = b.check()) return rc;
+    g.phase = axo::NORM_WHOLE;
+    return launch_norm_bwd(g, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_norm_bwd_part(const axo_problem_t* p, const void* dY, int64_t lddy, const void* S, int64_t lds, int type, const void* gamma,
+                      const float* stats, float* sums, float* dgamma, float* dbeta, int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    axo::NormBwdArgs g{};
+    Buffers b;
+    if (const int rc = plan_norm_bwd(p, dY, lddy, S, lds, type, gamma, stats, b, g)) return rc;
+    if (const int rc = first_error({check_vector(sums, g.K > 0 ? g.M : 0, 8, false), plan_norm_columns(dgamma, dbeta, accumulate, ws, ws_bytes, b, g)})) return rc;
+    b.writes(sums, 2 * (int64_t)g.M, 1, 2 * (int64_t)g.M, 4);
+    if (const int rc = b.check()) return rc;
+    g.sums = reinterpret_cast<float2*>(sums);
+    g.phase = axo::NORM_PART;
+    return launch_norm_bwd(g, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_norm_bwd_apply(const axo_problem_t* p, const void* dY, int64_t lddy, const void* S, int64_t lds, const void* R, int64_t ldr, int type,
+                       const void* gamma, const float* stats, const float* sums, void* dX, int64_t lddx, void* hip_stream) {
+    using namespace axo_block;
+    axo::NormBwdArgs g{};
+    Buffers b;
+    if (const int rc = plan_norm_bwd(p, dY, lddy, S, lds, type, gamma, stats, b, g)) return rc;
+    if (const int rc = first_error({check_vector(sums, g.K > 0 ? g.M : 0, 8, false), plan_norm_dx(R, ldr, type, dX, lddx, b, g)})) return rc;
+    b.reads(sums, 2 * (int64_t)g.M, 1, 2 * (int64_t)g.M, 4);
+    if (const int rc = b.check()) return rc;
+    g.sums = reinterpret_cast<float2*>(const_cast<float*>(sums));
+    g.phase = axo::NORM_APPLY;
+    return launch_norm_bwd(g, type, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t axo_norm_workspace_bytes(const axo_problem_t* p) {
+    axo_host::Shard s;
+    return axo_host::derive_shard(p, &s) ? 0 : axo_block::norm_workspace(s.M, s.Kl);
+}
+
+int axo_gated_fwd(const axo_problem_t* p, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, const void* bg, const void* bu,
+                  int gate, void* G, void* U, int64_t ldz, void* H, int64_t ldh, void* ws, size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    return guarded([&]() -> int {
+        Shard s;
+        if (const int rc = derive_shard(p, &s)) return rc;
+        if (!known_gate(gate)) return AXO_ERR_BAD_EPILOGUE;
+        const bool save = G || U;
+        const int64_t n = s.M > 0 ? s.Nl : 0;
+        if (const int rc = first_error({check_matrix(X, ldx, s.M, s.Kl), check_matrix(Wg, ldw, s.Kl, s.Nl), check_matrix(Wu, ldw, s.Kl, s.Nl),
+                                        check_vector(bg, n, 16, true), check_vector(bu, n, 16, true), check_matrix(H, ldh, s.M, s.Nl)}))
+            return rc;
+        if (save)
+            if (const int rc = first_error({check_matrix(G, ldz, s.M, s.Nl), check_matrix(U, ldz, s.M, s.Nl)})) return rc;
+        Buffers b;
+        b.reads(X, ldx, s.M, s.Kl, 2);
+        b.reads(Wg, ldw, s.Kl, s.Nl, 2);
+        b.reads(Wu, ldw, s.Kl, s.Nl, 2);
+        b.reads(bg, s.Nl, 1, s.Nl, 2);
+        b.reads(bu, s.Nl, 1, s.Nl, 2);
+        b.writes(H, ldh, s.M, s.Nl, 2);
+        if (save) {
+            b.writes(G, ldz, s.M, s.Nl, 2);
+            b.writes(U, ldz, s.M, s.Nl, 2);
+        }
+        if (const int rc = first_error({check_gated_workspace(s, ws, ws_bytes, b), b.check()})) return rc;
+        GatedArgs g{};
+        g.A = static_cast<const bf16_t*>(X); g.lda = ldx;
+        g.B = static_cast<const bf16_t*>(Wg); g.ldb = ldw;
+        g.B2 = static_cast<const bf16_t*>(Wu);
+        g.bias = s.k_coord == 0 ? static_cast<const bf16_t*>(bg) : nullptr;
+        g.bias2 = s.k_coord == 0 ? static_cast<const bf16_t*>(bu) : nullptr;
+        g.C = static_cast<bf16_t*>(H); g.ldc = ldh;
+        g.G = static_cast<bf16_t*>(G);
+        g.U = static_cast<bf16_t*>(U);
+        g.ldz = ldz;
+        g.Mo = (int)s.M; g.No = (int)s.Nl; g.R = (int)s.Kl;
+        g.gate = gate;
+        return launch_gated<axo::GATED_FWD>(g, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int axo_gated_act(const axo_problem_t* p, const void* G, const void* U, int64_t ldz, int gate, void* H, int64_t ldh, void* hip_stream) {
+    using namespace axo_block;
+    Shard s;
+    if (const int rc = derive_shard(p, &s)) return rc;
+    if (!known_gate(gate)) return AXO_ERR_BAD_EPILOGUE;
+    if (const int rc = first_error({check_matrix(G, ldz, s.M, s.Kl), check_matrix(U, ldz, s.M, s.Kl), check_matrix(H, ldh, s.M, s.Kl)})) return rc;
+    Buffers b;
+    b.reads(G, ldz, s.M, s.Kl, 2);
+    b.reads(U, ldz, s.M, s.Kl, 2);
+    b.writes(H, ldh, s.M, s.Kl, 2);
+    if (const int rc = b.check()) return rc;
+    axo::GatedMapArgs g{};
+    g.G = static_cast<const bf16_t*>(G);
+    g.U = static_cast<const bf16_t*>(U);
+    g.H = static_cast<bf16_t*>(H);
+    g.ldz = ldz;
+    g.ldout = ldh;
+    g.M = (int)s.M; g.N = (int)s.Kl;
+    g.gate = gate;
+    return launch_map(g, false, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_gated_dact(const axo_problem_t* p, const void* dH, int64_t lddh, const void* G, const void* U, int64_t ldz, int gate, void* dG, void* dU,
+                   int64_t lddz, void* hip_stream) {
+    using namespace axo_block;
+    Shard s;
+    if (const int rc = derive_shard(p, &s)) return rc;
+    if (!known_gate(gate)) return AXO_ERR_BAD_EPILOGUE;
+    if (const int rc = first_error({check_matrix(dH, lddh, s.M, s.Kl), check_matrix(G, ldz, s.M, s.Kl), check_matrix(U, ldz, s.M, s.Kl),
+                                    check_matrix(dG, lddz, s.M, s.Kl), check_matrix(dU, lddz, s.M, s.Kl)}))
+        return rc;
+    Buffers b;
+    b.reads(dH, lddh, s.M, s.Kl, 2);
+    b.reads(G, ldz, s.M, s.Kl, 2);
+    b.reads(U, ldz, s.M, s.Kl, 2);
+    b.writes(dG, lddz, s.M, s.Kl, 2);
+    b.writes(dU, lddz, s.M, s.Kl, 2);
+    if (const int rc = b.check()) return rc;
+    axo::GatedMapArgs g{};
+    g.dH = static_cast<const bf16_t*>(dH); g.lddh = lddh;
+    g.G = static_cast<const bf16_t*>(G);
+    g.U = static_cast<const bf16_t*>(U);
+    g.ldz = ldz;
+    g.dG = static_cast<bf16_t*>(dG);
+    g.dU = static_cast<bf16_t*>(dU);
+    g.ldout = lddz;
+    g.M = (int)s.M; g.N = (int)s.Kl;
+    g.gate = gate;
+    return launch_map(g, true, static_cast<hipStream_t>(hip_stream));
+}
+
+int axo_gated_dgrad_act(const axo_problem_t* p, const void* dY, int64_t lddy, const void* W, int64_t ldw, const void* G, const void* U, int64_t ldz,
+                        int gate, void* dG, void* dU, int64_t lddz, void* ws, size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    return guarded([&]() -> int {
+        Shard s;
+        if (const int rc = derive_shard(p, &s)) return rc;
+        if (!known_gate(gate)) return AXO_ERR_BAD_EPILOGUE;
+        if (const int rc = first_error({check_matrix(dY, lddy, s.M, s.Nl), check_matrix(W, ldw, s.Kl, s.Nl), check_matrix(G, ldz, s.M, s.Kl),
+                                        check_matrix(U, ldz, s.M, s.Kl), check_matrix(dG, lddz, s.M, s.Kl), check_matrix(dU, lddz, s.M, s.Kl)}))
+            return rc;
+        Buffers b;
+        b.reads(dY, lddy, s.M, s.Nl, 2);
+        b.reads(W, ldw, s.Kl, s.Nl, 2);
+        b.reads(G, ldz, s.M, s.Kl, 2);
+        b.reads(U, ldz, s.M, s.Kl, 2);
+        b.writes(dG, lddz, s.M, s.Kl, 2);
+        b.writes(dU, lddz, s.M, s.Kl, 2);
+        if (const int rc = first_error({check_gated_workspace(s, ws, ws_bytes, b), b.check()})) return rc;
+        GatedArgs g{};
+        g.A = static_cast<const bf16_t*>(dY); g.lda = lddy;
+        g.B = static_cast<const bf16_t*>(W); g.ldb = ldw;
+        g.C = static_cast<bf16_t*>(dG); g.ldc = lddz;
+        g.U = static_cast<bf16_t*>(dU);
+        g.aux = static_cast<const bf16_t*>(G); g.ldaux = ldz;
+        g.aux2 = static_cast<const bf16_t*>(U);
+        g.Mo = (int)s.M; g.No = (int)s.Kl; g.R = (int)s.Nl;
+        g.gate = gate;
+        return launch_gated<axo::GATED_DACT>(g, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int axo_gated_dgrad(const axo_problem_t* p, const void* dG, const void* dU, int64_t lddz, const void* Wg, const void* Wu, int64_t ldw, void* dX,
+                    int64_t lddx, void* ws, size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    return guarded([&]() -> int {
+        Shard s;
+        if (const int rc = derive_shard(p, &s)) return rc;
+        if (const int rc = first_error({check_matrix(dG, lddz, s.M, s.Nl), check_matrix(dU, lddz, s.M, s.Nl), check_matrix(Wg, ldw, s.Kl, s.Nl),
+                                        check_matrix(Wu, ldw, s.Kl, s.Nl), check_matrix(dX, lddx, s.M, s.Kl)}))
+            return rc;
+        Buffers b;
+        b.reads(dG, lddz, s.M, s.Nl, 2);
+        b.reads(dU, lddz, s.M, s.Nl, 2);
+        b.reads(Wg, ldw, s.Kl, s.Nl, 2);
+        b.reads(Wu, ldw, s.Kl, s.Nl, 2);
+        b.writes(dX, lddx, s.M, s.Kl, 2);
+        if (const int rc = first_error({check_gated_workspace(s, ws, ws_bytes, b), b.check()})) return rc;
+        GatedArgs g{};
+        g.A = static_cast<const bf16_t*>(dG); g.lda = lddz;
+        g.A2 = static_cast<const bf16_t*>(dU);
+        g.B = static_cast<const bf16_t*>(Wg); g.ldb = ldw;
+        g.B2 = static_cast<const bf16_t*>(Wu);
+        g.C = static_cast<bf16_t*>(dX); g.ldc = lddx;
+        g.Mo = (int)s.M; g.No = (int)s.Kl; g.R = (int)s.Nl;
+        return launch_gated<axo::GATED_DX>(g, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int axo_gated_wgrad(const axo_problem_t* p, const void* X, int64_t ldx, const void* dG, const void* dU, int64_t lddz, void* dWg, void* dWu,
+                    int64_t lddw, void* ws, size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    return guarded([&]() -> int {
+        return gated_wgrad(p, X, ldx, dG, dU, lddz, static_cast<bf16_t*>(dWg), static_cast<bf16_t*>(dWu), lddw, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int axo_gated_wgrad_acc(const axo_problem_t* p, const void* X, int64_t ldx, const void* dG, const void* dU, int64_t lddz, float* dWg, float* dWu,
+                        int64_t lddw, void* ws, size_t ws_bytes, void* hip_stream) {
+    using namespace axo_block;
+    return guarded([&]() -> int { return gated_wgrad(p, X, ldx, dG, dU, lddz, dWg, dWu, lddw, ws, ws_bytes, static_cast<hipStream_t>(hip_stream)); });
+}
+
+size_t axo_gated_workspace_bytes(const axo_problem_t* p) {
+    axo_host::Shard s;
+    return axo_host::derive_shard(p, &s) ? 0 : axo_block::gated_workspace(s);
+}
+
+}  // extern "C"

@@ -1,0 +1,293 @@
+"""Layer norm on the GPU, forward and backward, whole and in halves over a split width, against the 64-bit definition."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import block_util as bu
+import paper_2305_13525_amd as axo
+from oracle import block as ob
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+# rows x columns: one value, below and around a wave, a power of two either side, odd lengths, rows past what fits registers
+SIZES = [(1, 1), (1, 8), (3, 7), (2, 9), (5, 33), (70, 64), (2, 65), (130, 127), (17, 128), (4, 250), (9, 256), (2, 257), (5, 512), (3, 513), (33, 1000),
+         (4, 1024), (35, 1027), (2, 2048), (3, 2056), (1, 4096), (300, 4096), (2, 4099), (3, 7168), (2, 8192), (2, 9000), (3, 12288), (2, 16384),
+         (2, 16385), (2, 20000), (1, 32768), (2, 33001)]
+
+
+def inputs(m, k, wide, seed, mean=0.3):
+    rng = np.random.default_rng(seed)
+    d = {"x": bu.draw(rng, m, k, 1.5, mean, wide), "r": bu.draw(rng, m, k, 1.0, 0.0, wide), "dy": bu.draw(rng, m, k),
+         "gamma": bu.draw(rng, 1, k, 0.2, 1.0)[0], "beta": bu.draw(rng, 1, k, 0.2)[0]}
+    return d
+
+
+def stored(a, wide):
+    """Rounded once to the stream's type (fp32 sums of bf16 values and their rounding to bf16 included)."""
+    t = torch.from_numpy(a).float()
+    return (t if wide else t.bfloat16()).double().numpy()
+
+
+def forward(d, wide, res, gap=0, gamma=True, beta=True, stats=True, eps=EPS):
+    m, k = d["x"].shape
+    p = bu.problem(m, k, 0)
+    X, R = bu.Mat(d["x"], gap, wide), bu.Mat(d["r"], gap + 8, wide) if res else None
+    S, Y = bu.Out(m, k, gap, wide) if res else None, bu.Out(m, k, gap)
+    st = torch.full((m, 2), float("nan"), device=bu.DEV) if stats else None
+    gm, bt = bu.vec(d["gamma"]) if gamma else None, bu.vec(d["beta"]) if beta else None
+    axo.axo_norm_fwd(p, X.ptr, X.ld, bu.ptr(R), R.ld if res else 0, int(wide), bu.ptr(gm), bu.ptr(bt), eps, bu.ptr(S), S.ld if res else 0, Y.ptr, Y.ld,
+                     bu.ptr(st), bu.stream())
+    torch.cuda.synchronize()
+    return S.result() if res else None, Y.result(), None if st is None else st.double().cpu().numpy()
+
+
+def check_forward(d, wide, res, gap=0, gamma=True, beta=True, eps=EPS):
+    S, Y, st = forward(d, wide, res, gap, gamma, beta, True, eps)
+    s = d["x"] + d["r"] if res else d["x"]
+    if res:
+        want = stored(s, wide)
+        assert np.array_equal(S, want)
+        s = want
+    gm, bt = d["gamma"] if gamma else None, d["beta"] if beta else None
+    y, mean, rstd = ob.norm_fwd(s, gm, bt, eps)
+    by, bm, br = bu.norm_bounds(s, mean, rstd, gm, bt, y, wide)
+    bu.within(st[:, 0], mean, bm, "mean")
+    bu.within(st[:, 1], rstd, br, "rstd")
+    bu.within(Y, y, by, "y")
+
+
+@pytest.mark.parametrize("m,k", SIZES)
+@pytest.mark.parametrize("wide", [False, True])
+def test_forward(m, k, wide):
+    d = inputs(m, k, wide, 100 * m + k)
+    check_forward(d, wide, res=False)
+    check_forward(d, wide, res=True, gap=8)
+
+
+@pytest.mark.parametrize("gamma,beta", [(False, False), (True, False), (False, True)])
+def test_forward_without_weights(gamma, beta):
+    for m, k in ((3, 100), (2, 4104)):
+        check_forward(inputs(m, k, False, 7), False, True, 8, gamma, beta)
+
+
+def test_forward_far_from_zero():
+    """A mean a thousand deviations from zero: the variance comes from deviations, not from squares."""
+    for k in (64, 1000, 5000, 33000):
+        check_forward(inputs(4, k, True, 8, mean=1000.0), True, False)
+
+
+def test_constant_rows_and_eps():
+    d = inputs(3, 200, False, 9)
+    d["x"][:] = 2.5
+    _, y, st = forward(d, False, False)
+    assert np.array_equal(y, np.broadcast_to(d["beta"], y.shape)) and np.array_equal(st[:, 0], [2.5] * 3)
+    bu.within(st[:, 1], np.full(3, EPS ** -0.5), 1e-4)
+    check_forward(inputs(3, 200, False, 10), False, False, eps=0.0)
+    check_forward(inputs(3, 200, False, 10), False, False, eps=3.0)
+
+
+def test_infinities_and_nans_stay_in_their_rows():
+    for k in (40, 1000, 4096, 12288, 33000):
+        d = inputs(6, k, False, 11)
+        clean = forward(d, False, False)
+        d["x"][1, k // 2], d["x"][4, 0] = np.inf, np.nan
+        got = forward(d, False, False)
+        for row in range(6):
+            if row in (1, 4):
+                assert np.isnan(got[1][row]).all()
+            else:
+                assert np.array_equal(got[1][row], clean[1][row]) and np.array_equal(got[2][row], clean[2][row])
+
+
+def backward(d, wide, res, gap=0, gamma=True, which=(True, True), acc=None):
+    m, k = d["x"].shape
+    _, mean, rstd = ob.norm_fwd(d["x"], eps=EPS) if m and k else (None, np.zeros(m), np.ones(m))
+    st = torch.from_numpy(np.stack([mean, rstd], 1)).float().to(bu.DEV)
+    mean, rstd = st.double().cpu().numpy().T if m else (mean, rstd)
+    p = bu.problem(m, k, 0)
+    dY, X, R = bu.Mat(d["dy"], gap), bu.Mat(d["x"], gap + 16, wide), bu.Mat(d["r"], gap, wide) if res else None
+    dX = bu.Out(m, k, gap + 8, wide)
+    start = np.zeros(k) if acc is None else acc
+    dg, db = (torch.from_numpy(start if acc is not None else np.full(k, np.nan)).float().to(bu.DEV) if w else None for w in which)
+    gm = bu.vec(d["gamma"]) if gamma else None
+    n = axo.axo_norm_workspace_bytes(p)
+    ws = torch.full((max(n, 16),), 255, dtype=torch.uint8, device=bu.DEV)
+    axo.axo_norm_bwd(p, dY.ptr, dY.ld, X.ptr, X.ld, bu.ptr(R), R.ld if res else 0, int(wide), bu.ptr(gm), st.data_ptr(), dX.ptr, dX.ld, bu.ptr(dg),
+                     bu.ptr(db), int(acc is not None), ws.data_ptr(), n, bu.stream())
+    torch.cuda.synchronize()
+    back = lambda t: None if t is None else t.double().cpu().numpy()  # noqa: E731
+    return mean, rstd, dX.result(), back(dg), back(db)
+
+
+def check_backward(d, wide, res, gap=0, gamma=True, which=(True, True), acc=None):
+    mean, rstd, dx, dg, db = backward(d, wide, res, gap, gamma, which, acc)
+    gm, r = d["gamma"] if gamma else None, d["r"] if res else None
+    want = ob.norm_bwd(d["dy"], d["x"], mean, rstd, gm, r)
+    bounds = bu.norm_bwd_bounds(d["dy"], d["x"], mean, rstd, gm, r, want[0], wide)
+    bu.within(dx, want[0], bounds[0], "dx")
+    start = 0.0 if acc is None else acc
+    for got, w, bound, name in ((dg, want[1], bounds[1], "dgamma"), (db, want[2], bounds[2], "dbeta")):
+        if got is not None:
+            bu.within(got, w + start, bound + bu.FP32 * np.abs(w + start) * 2, name)
+
+
+@pytest.mark.parametrize("m,k", SIZES + [(513, 40), (1030, 100), (5000, 72), (700, 1100)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_backward(m, k, wide):
+    d = inputs(m, k, wide, 200 * m + k)
+    check_backward(d, wide, res=False)
+    check_backward(d, wide, res=True, gap=8)
+
+
+def test_backward_parts_of_it():
+    for m, k in ((5, 100), (300, 1032), (2, 17000)):
+        d = inputs(m, k, False, 12)
+        check_backward(d, False, True, 0, gamma=False)
+        check_backward(d, False, False, 0, which=(True, False))
+        check_backward(d, False, False, 0, which=(False, True))
+        check_backward(d, False, False, 0, which=(False, False))
+        check_backward(d, False, False, 0, acc=np.linspace(-3, 3, k).astype(np.float32).astype(np.float64))
+
+
+def test_no_rows():
+    """Sums over no rows are zero, or what was there."""
+    d = {k: v[:0] if v.ndim == 2 else v for k, v in inputs(3, 50, False, 13).items()}
+    *_, dg, db = backward(d, False, False)
+    assert not dg.any() and not db.any()
+    start = np.arange(50.0)
+    *_, dg, db = backward(d, False, False, acc=start)
+    assert np.array_equal(dg, start) and np.array_equal(db, start)
+
+
+def test_backward_against_differences():
+    """The gradient of sum(y * c) along a direction, from central differences of the 64-bit forward pass."""
+    m, k = 7, 96
+    d = inputs(m, k, True, 14)
+    rng = np.random.default_rng(15)
+    v, vg, vb = rng.standard_normal((m, k)), rng.standard_normal(k), rng.standard_normal(k)
+    _, _, dx, dg, db = backward(d, True, False)
+    loss = lambda t: (ob.norm_fwd(d["x"] + t * v, d["gamma"] + t * vg, d["beta"] + t * vb, EPS)[0] * d["dy"]).sum()  # noqa: E731
+    step = 1e-5
+    slope = (loss(step) - loss(-step)) / (2 * step)
+    parts = np.array([(dx * v).sum(), (dg * vg).sum(), (db * vb).sum()])
+    scale = np.abs(dx * v).sum() + np.abs(dg * vg).sum() + np.abs(db * vb).sum()
+    assert abs(parts.sum() - slope) <= 1e-5 * scale  # fp32 statistics and sums
+
+
+@pytest.mark.parametrize("transposed", [0, 1])
+@pytest.mark.parametrize("k,parts", [(96, 2), (2048, 4), (3000, 3), (24, 1), (66000, 2)])
+def test_split_width(k, parts, transposed):
+    """The halves of a norm on every shard of a split width, in place in the whole matrices, joined on the test's side."""
+    m, kl = 9, k // parts
+    if kl % 8:
+        k = parts * 8 * max(1, kl // 8)
+        kl = k // parts
+    d = inputs(m, k, False, 16)
+    s = stored(d["x"] + d["r"], False)
+    X, R, dY, dR = bu.Mat(d["x"]), bu.Mat(d["r"]), bu.Mat(d["dy"]), bu.Mat(d["r"])
+    S, Y, dX = bu.Out(m, k), bu.Out(m, k), bu.Out(m, k)
+    gm, bt = bu.vec(d["gamma"]), bu.vec(d["beta"])
+    st = torch.full((m, 2), float("nan"), device=bu.DEV)
+    gathered = torch.full((parts, m, 2), float("nan"), device=bu.DEV)
+    grid = (1, parts, 1) if transposed else (parts, 1, 1)
+    shard = lambda i: bu.problem(m, k, 0, grid, (0, i, 0) if transposed else (i, 0, 0), transposed)  # noqa: E731
+    for i in range(parts):
+        at = i * kl * 2
+        axo.axo_norm_part(shard(i), X.ptr + at, X.ld, R.ptr + at, R.ld, 0, S.ptr + at, S.ld, gathered[i].data_ptr(), bu.stream())
+    for i in range(parts):
+        at = i * kl * 2
+        axo.axo_norm_apply(shard(i), S.ptr + at, S.ld, 0, gathered.data_ptr(), parts, gm.data_ptr() + at, bt.data_ptr() + at, EPS, Y.ptr + at, Y.ld,
+                           st.data_ptr(), bu.stream())
+    torch.cuda.synchronize()
+    assert np.array_equal(S.result(), s)
+    y, mean, rstd = ob.norm_fwd(s, d["gamma"], d["beta"], EPS)
+    by, bm, br = bu.norm_bounds(s, mean, rstd, d["gamma"], d["beta"], y, False)
+    got = st.double().cpu().numpy()
+    bu.within(got[:, 0], mean, bm, "mean")
+    bu.within(got[:, 1], rstd, br, "rstd")
+    bu.within(Y.result(), y, by, "y")
+
+    sums = torch.zeros((parts, m, 2), device=bu.DEV)
+    dg, db = torch.full((k,), float("nan"), device=bu.DEV), torch.full((k,), float("nan"), device=bu.DEV)
+    for i in range(parts):
+        at, n = i * kl * 2, axo.axo_norm_workspace_bytes(shard(i))
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=bu.DEV)
+        axo.axo_norm_bwd_part(shard(i), dY.ptr + at, dY.ld, S.ptr + at, S.ld, 0, gm.data_ptr() + at, st.data_ptr(), sums[i].data_ptr(),
+                              dg.data_ptr() + 2 * at, db.data_ptr() + 2 * at, 0, ws.data_ptr(), n, bu.stream())
+    total = sums.sum(0)
+    for i in range(parts):
+        at = i * kl * 2
+        axo.axo_norm_bwd_apply(shard(i), dY.ptr + at, dY.ld, S.ptr + at, S.ld, dR.ptr + at, dR.ld, 0, gm.data_ptr() + at, st.data_ptr(),
+                               total.data_ptr(), dX.ptr + at, dX.ld, bu.stream())
+    torch.cuda.synchronize()
+    want = ob.norm_bwd(d["dy"], s, got[:, 0], got[:, 1], d["gamma"], d["r"])
+    bounds = bu.norm_bwd_bounds(d["dy"], s, got[:, 0], got[:, 1], d["gamma"], d["r"], want[0], False)
+    bu.within(dX.result(), want[0], bounds[0], "dx")
+    bu.within(dg.double().cpu().numpy(), want[1], bounds[1], "dgamma")
+    bu.within(db.double().cpu().numpy(), want[2], bounds[2], "dbeta")
+
+
+def test_offsets_past_32_bits():
+    """Rows a billion elements apart."""
+    m, k, ld = 3, 1000, (1 << 30) + 8
+    d = inputs(m, k, False, 17)
+    whole = torch.empty(2 * ld + 1024, dtype=torch.bfloat16, device=bu.DEV)
+    rows = whole.as_strided((m, k), (ld, 1))
+    rows.copy_(torch.from_numpy(d["x"]).bfloat16())
+    Y = torch.full((2 * ld + 1024,), float("nan"), dtype=torch.bfloat16, device=bu.DEV)
+    st = torch.empty((m, 2), device=bu.DEV)
+    gm, bt = bu.vec(d["gamma"]), bu.vec(d["beta"])
+    p = bu.problem(m, k, 0)
+    axo.axo_norm_fwd(p, whole.data_ptr(), ld, None, 0, 0, gm.data_ptr(), bt.data_ptr(), EPS, None, 0, Y.data_ptr(), ld, st.data_ptr(), bu.stream())
+    y, mean, rstd = ob.norm_fwd(d["x"], d["gamma"], d["beta"], EPS)
+    bu.within(Y.as_strided((m, k), (ld, 1)).double().cpu().numpy(), y, bu.norm_bounds(d["x"], mean, rstd, d["gamma"], d["beta"], y, False)[0])
+    dY, dX = bu.Mat(d["dy"]), Y
+    ws = torch.empty(axo.axo_norm_workspace_bytes(p), dtype=torch.uint8, device=bu.DEV)
+    dg = torch.empty(k, device=bu.DEV)
+    axo.axo_norm_bwd(p, dY.ptr, dY.ld, whole.data_ptr(), ld, None, 0, 0, gm.data_ptr(), st.data_ptr(), dX.data_ptr(), ld, dg.data_ptr(), None, 0,
+                     ws.data_ptr(), ws.numel(), bu.stream())
+    s2 = st.double().cpu().numpy()
+    want = ob.norm_bwd(d["dy"], d["x"], s2[:, 0], s2[:, 1], d["gamma"])
+    bounds = bu.norm_bwd_bounds(d["dy"], d["x"], s2[:, 0], s2[:, 1], d["gamma"], None, want[0], False)
+    bu.within(dX.as_strided((m, k), (ld, 1)).double().cpu().numpy(), want[0], bounds[0])
+    bu.within(dg.double().cpu().numpy(), want[1], bounds[1])
+
+
+@pytest.mark.parametrize("m,k", [(1, 4096), (37, 1027), (700, 512), (64, 12288), (3, 33000)])
+def test_same_bits_on_any_stream_and_in_graphs(m, k):
+    d = inputs(m, k, False, 18)
+    first, again = backward(d, False, True), None
+    fwd = forward(d, False, True)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        again = backward(d, False, True)
+        fwd2 = forward(d, False, True)
+    assert all(np.array_equal(a, b) for a, b in zip(first, again)) and all(np.array_equal(a, b) for a, b in zip(fwd, fwd2))
+
+    p = bu.problem(m, k, 0)
+    X, dY, Y, dX = bu.Mat(d["x"]), bu.Mat(d["dy"]), bu.Out(m, k), bu.Out(m, k)
+    gm, bt, st = bu.vec(d["gamma"]), bu.vec(d["beta"]), torch.zeros((m, 2), device=bu.DEV)
+    dg, db = torch.zeros(k, device=bu.DEV), torch.zeros(k, device=bu.DEV)
+    ws = torch.empty(max(16, axo.axo_norm_workspace_bytes(p)), dtype=torch.uint8, device=bu.DEV)
+
+    def both():
+        axo.axo_norm_fwd(p, X.ptr, X.ld, None, 0, 0, gm.data_ptr(), bt.data_ptr(), EPS, None, 0, Y.ptr, Y.ld, st.data_ptr(), bu.stream())
+        axo.axo_norm_bwd(p, dY.ptr, dY.ld, X.ptr, X.ld, None, 0, 0, gm.data_ptr(), st.data_ptr(), dX.ptr, dX.ld, dg.data_ptr(), db.data_ptr(), 0,
+                         ws.data_ptr(), ws.numel(), bu.stream())
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for turn in range(3):
+        X.view().copy_(torch.from_numpy(np.roll(d["x"], turn, axis=0)).bfloat16())
+        both()
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in (Y.view(), dX.view(), dg, db, st)]
+        for t in (Y.flat, dX.flat, dg, db, st):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (Y.view(), dX.view(), dg, db, st))), turn
