@@ -187,7 +187,6 @@ int launch_tiles(void (*kern)(GemmArgs, int, int, int), std::atomic<uint64_t>* r
 // dgrad 7.3 / 7.0, wgrad 7.4 / 6.8, wgrad 2000 x 1000 of 512 tokens 7.8 / 6.75, dgrad 6.15 / 6.0.  Of the two kinds the one with fewer tiles, else the
 // wide one, which reads the rows of a forward's W in segments of 256 bytes (1000 x 2000 x 3000 19.7 us, 20.1 on the tall ones, dgrad 17.9 and 18.2,
 // wgrad either way 21.0; wgrad 900 x 1300 of 6000 38.3 and 36.5).
-enum class Tiles { small, wide, tall, mid, big };
 Tiles tiles_of(int Mo, int No, int R) {
     const int64_t wide = tiles_in(Mo, 64) * tiles_in(No, 128), tall = tiles_in(Mo, 128) * tiles_in(No, 64);
     if (std::min(wide, tall) <= NUM_CU && 8 * tiles_in(Mo, 64) * tiles_in(No, 64) > 9 * NUM_CU && steps_in(R) >= 16) return wide <= tall ? Tiles::wide : Tiles::tall;
@@ -1279,7 +1278,13 @@ int launch_products(const GemmArgs* products, int n, int la, int lb, hipStream_t
     return by_level(plans, std::vector<int>((size_t)n, 0), 1, Enqueue{st});
 }
 
-axo::TileSched plan_columns(int Mo, int No) { return plan_tiles(Mo, No); }
+Tiles quickest_tiles(int Mo, int No, int R) { return tiles_of(Mo, No, R); }
+
+axo::TileSched plan_columns(int Mo, int No, int R) {
+    axo::TileSched sc = plan_tiles(Mo, No);
+    sc.shift = shift_units(Mo, No, R);
+    return sc;
+}
 
 }  // namespace axo_host
 

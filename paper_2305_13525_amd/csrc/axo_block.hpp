@@ -197,10 +197,51 @@ int launch_gated_generic(const GatedArgs& g, hipStream_t st) {
     hipLaunchKernelGGL(axo::gated_generic_kernel<OP>, grid, dim3(256), 0, st, g);
     return launched();
 }
+// Byte offsets inside an operand of a tile are formed in 32 bits (spans_ok of the products): 256 rows of a KC operand, the walked reduction of an MC one.
+template <int OP>
+bool gated_spans_ok(const GatedArgs& g) {
+    auto fits = [](int64_t elems) { return elems * 2 < (int64_t)0xFFFF0000; };
+    const int64_t walked = ((int64_t)g.R + 2 * axo::TILE_BK - 1) / (2 * axo::TILE_BK) * (2 * axo::TILE_BK);
+    return fits(256 * g.lda + walked) && fits(OP == axo::GATED_FWD ? walked * g.ldb + 256 : 256 * g.ldb + walked);
+}
+
+// Rows of the outputs that straddle cache lines are stored plainly (store_row).
+template <int OP>
+bool gated_plain(const GatedArgs& g) {
+    auto straddles = [](const void* p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 2)) & 127) != 0; };
+    return straddles(g.C, g.ldc);
+}
+
+template <typename C, int OP, typename Kernel>
+int launch_gated_tiles(Kernel kern, std::atomic<uint64_t>* raised, const GatedArgs& g, int rows, int cols, hipStream_t st) {
+    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), C::LDS_BYTES, raised)) return AXO_ERR_HIP;
+    axo::GatedProduct<OP> args{g};
+    const int tm = (int)tiles_in(g.Mo, rows), tn = (int)tiles_in(g.No, axo::gated_cols<OP>(cols));
+    hipLaunchKernelGGL(kern, dim3((unsigned)tm * (unsigned)tn), dim3(C::THREADS), C::LDS_BYTES, st, args, tm, tn, std::min(tm, 8));
+    return launched();
+}
+template <int OP, bool PLAIN>
+int launch_gated_on(const GatedArgs& g, Tiles tiles, int cols, int steps, hipStream_t st) {
+    static std::atomic<uint64_t> raised[4]{{0}, {0}, {0}, {0}};
+    if (tiles == Tiles::small) return launch_gated_tiles<axo::SmallCfg<false>, OP>(axo::gated_small_kernel<OP, PLAIN>, &raised[0], g, 64, 64, st);
+    if (tiles == Tiles::wide) return launch_gated_tiles<axo::RectCfg<true>, OP>(axo::gated_rect_kernel<OP, PLAIN>, &raised[1], g, 64, 128, st);
+    if (tiles == Tiles::mid) return launch_gated_tiles<axo::MidCfg, OP>(axo::gated_mid_kernel<OP, PLAIN>, &raised[2], g, 128, 128, st);
+    auto kern = axo::gated_mixed_kernel<OP, PLAIN>;
+    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), axo::MIX_LDS_BYTES, &raised[3])) return AXO_ERR_HIP;
+    const axo::TileSched sc = plan_columns(g.Mo, cols, steps);
+    hipLaunchKernelGGL(kern, dim3(sc.n_big + sc.tiles_m * sc.small_cols), dim3(axo::TILE_THREADS), axo::MIX_LDS_BYTES, st, axo::GatedProduct<OP>{g}, sc);
+    return launched();
+}
 template <int OP>
 int launch_gated(const GatedArgs& g, hipStream_t st) {
     if (g.Mo == 0 || g.No == 0) return AXO_OK;
-    return launch_gated_generic<OP>(g, st);
+    // as one product: twice the columns, or twice the reduction
+    const int64_t cols = OP == axo::GATED_FWD ? 2 * (int64_t)g.No : g.No, red = OP == axo::GATED_DX ? 2 * (int64_t)g.R : g.R;
+    if (g.R == 0 || !gated_spans_ok<OP>(g) || cols > INT32_MAX || red > INT32_MAX || !grid_fits(tiles_in(g.Mo, 64) * tiles_in((int)cols, 64), axo::TILE_THREADS))
+        return launch_gated_generic<OP>(g, st);
+    Tiles tiles = quickest_tiles(g.Mo, (int)cols, (int)red);
+    if (tiles == Tiles::tall) tiles = tiles_in(g.Mo, 64) * tiles_in((int)cols, 128) <= NUM_CU ? Tiles::wide : Tiles::mid;
+    return gated_plain<OP>(g) ? launch_gated_on<OP, true>(g, tiles, (int)cols, (int)red, st) : launch_gated_on<OP, false>(g, tiles, (int)cols, (int)red, st);
 }
 
 size_t gated_workspace(const Shard&) { return 0; }

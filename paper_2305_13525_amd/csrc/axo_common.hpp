@@ -29,8 +29,15 @@ enum Epilogue {
     EPI_MUL_DGELU_TANH = 4, EPI_MUL_DGELU_ERF = 5, EPI_ACC_F32 = 6
 };
 
+// What a tile computes besides one product with the epilogues above: the products of a gated block (gated.hpp).
+//   GATED_FWD   two products with the same A in one tile, the columns of B and B2 beside each other; act(first) * second
+//   GATED_DACT  one product, taken through the derivative of that
+//   GATED_DX    the sum of two products, A B^T + A2 B2^T
+enum GatedOp { NOT_GATED = -1, GATED_FWD = 0, GATED_DACT = 1, GATED_DX = 2 };
+
 // One GEMM as the kernels see it.
 struct GemmArgs {
+    static constexpr int OP = NOT_GATED;
     const bf16_t* A; int64_t lda;
     const bf16_t* B; int64_t ldb;
     bf16_t* C;       int64_t ldc;   // EPI_ACC_F32: C points to fp32 and ldc counts fp32 elements
@@ -143,5 +150,23 @@ __device__ __forceinline__ float apply_epilogue(float acc, float b, int epi) {
 __device__ __forceinline__ float apply_dact(float acc, float p, int epi) {
     return acc * (epi == EPI_MUL_DGELU_TANH ? dgelu_tanh(p) : dgelu_erf(p));
 }
+
+// What the kernels of a gated block take beside a product's arguments.
+enum Gate { GATE_SILU = 0, GATE_GELU_TANH = 1, GATE_GELU_ERF = 2 };
+struct GatedArgs : GemmArgs {
+    const bf16_t* A2;     // dU, of dX
+    const bf16_t* B2;     // Wu
+    const bf16_t* bias2;  // bu
+    const bf16_t* aux2;   // U, where aux is G (their pitch: ldaux)
+    bf16_t* G;            // outputs beside C: G and U of the forward pass or nullptr, pitch ldz
+    bf16_t* U;            // ... dU of the backward pass, where C is dG (pitch ldc)
+    int64_t ldz;
+    int gate;             // Gate
+};
+// The same, for tiles that do OP_.
+template <int OP_>
+struct GatedProduct : GatedArgs {
+    static constexpr int OP = OP_;
+};
 
 }  // namespace axo

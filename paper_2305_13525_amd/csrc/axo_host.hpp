@@ -133,7 +133,10 @@ int guarded(F&& body) noexcept {
 
 // Independent products of one kind, in as few launches as a chain's level takes (defined beside the chain's planner).
 int launch_products(const axo::GemmArgs* products, int n, int la, int lb, hipStream_t st);
-// How an output of 256-row tiles is cut into columns of whole and of half-width tiles (defined beside the planners).
-axo::TileSched plan_columns(int Mo, int No);
+// The tiles of a product on its own, whichever are estimated quickest, from its sizes alone, and how an output of 256-row tiles is cut into columns of whole and of
+// half-width ones, start-up shift included (defined beside the planners).
+enum class Tiles { small, wide, tall, mid, big };
+Tiles quickest_tiles(int Mo, int No, int R);
+axo::TileSched plan_columns(int Mo, int No, int R);
 
 }  // namespace axo_host

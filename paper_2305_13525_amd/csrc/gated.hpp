@@ -2,55 +2,15 @@
 //   dG = dH U act'(G), dU = dH act(G)          dH = dY W^T of the layer behind the block
 //   dX = dG Wg^T + dU Wu^T                     one reduction over both products
 //   dWg = X^T dG, dWu = X^T dU                 two weight gradients (gemm_tile.hpp, gemm_slim.hpp)
-// This file: the activations, the element-wise forms and kernels for operands whose spans pass 4 GiB.
+// This file: the element-wise forms and kernels for operands whose spans pass 4 GiB.
 #pragma once
 #include "axo_common.hpp"
+#include "gate.hpp"
 #include "gemm_generic.hpp"
+#include "gemm_tile.hpp"
 #include "norm.hpp"
 
 namespace axo {
-
-enum Gate { GATE_SILU = 0, GATE_GELU_TANH = 1, GATE_GELU_ERF = 2 };
-
-// v sigmoid(v): one exp2 and one reciprocal, as gelu_tanh.  Below v = -87 exp(-v) passes 2^126 and the result is zero (it is smaller than 2^-119).
-__device__ __forceinline__ float silu(float v) {
-    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.4426950408889634f));
-}
-template <int GATE>
-__device__ __forceinline__ float gate_value(float v) {
-    return GATE == GATE_SILU ? silu(v) : GATE == GATE_GELU_TANH ? gelu_tanh(v) : gelu_erf(v);
-}
-// The value and its derivative.
-template <int GATE>
-__device__ __forceinline__ float2 gate_both(float v) {
-    if (GATE == GATE_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.4426950408889634f));
-        return float2{v * s, s * __builtin_fmaf(v, 1.0f - s, 1.0f)};
-    }
-    // beyond 16 the derivative is that of 16 (1 or 0, and nothing overflows on the way); NaN stays NaN
-    if (GATE == GATE_GELU_TANH) return float2{gelu_tanh(v), dgelu_tanh(v > 16.0f ? 16.0f : v < -16.0f ? -16.0f : v)};
-    return float2{gelu_erf(v), dgelu_erf(v)};
-}
-
-// What the kernels of the block take beside a product's arguments.
-struct GatedArgs : GemmArgs {
-    const bf16_t* A2;     // dU, of dX
-    const bf16_t* B2;     // Wu
-    const bf16_t* bias2;  // bu
-    const bf16_t* aux2;   // U, where aux is G (their pitch: ldaux)
-    bf16_t* G;            // outputs beside C: G and U of the forward pass or nullptr, pitch ldz
-    bf16_t* U;            // ... dU of the backward pass, where C is dG (pitch ldc)
-    int64_t ldz;
-    int gate;             // Gate
-};
-
-// f of the gate as a compile-time constant.
-template <typename F>
-__device__ __forceinline__ void with_gate(int gate, F f) {
-    if (gate == GATE_SILU) f(std::integral_constant<int, GATE_SILU>{});
-    else if (gate == GATE_GELU_TANH) f(std::integral_constant<int, GATE_GELU_TANH>{});
-    else f(std::integral_constant<int, GATE_GELU_ERF>{});
-}
 
 // H = act(G) * U, eight columns of a row per thread and turn.
 struct GatedMapArgs {
@@ -92,7 +52,6 @@ __global__ void __launch_bounds__(GATED_MAP_THREADS) gated_map_kernel(GatedMapAr
 
 // The block's products for any sizes and spans, 64-bit indices, 128 x 128 tiles staged through registers as gemm_generic_kernel: what is left to it are
 // empty reductions and operands whose spans pass 4 GiB.
-enum GatedOp { GATED_FWD = 0, GATED_DACT = 1, GATED_DX = 2 };
 template <int OP>
 __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
     constexpr int LB = OP == GATED_FWD ? MC : KC, SUMS = OP == GATED_FWD ? 2 : 1;
@@ -168,6 +127,55 @@ __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
                 }
             }
     });
+}
+
+// ---- the block's products on the tiles of gemm_tile.hpp ---------------------------------------
+// The forward's tiles hold as many columns of Wg as of Wu, so a tile of BN columns of the two is one of BN / 2 columns of H, and the operands are read and the
+// matrix units fed as for one product of twice the columns.  dX is one product of twice the reduction.
+template <int OP>
+constexpr int GATED_LB = OP == GATED_FWD ? MC : KC;
+template <int OP>
+constexpr int gated_cols(int BN) { return OP == GATED_FWD ? BN / 2 : BN; }  // of the output, in a tile of BN columns of B
+
+template <int OP, bool PLAIN>
+__global__ void __launch_bounds__(TILE_THREADS, 1) gated_mixed_kernel(GatedProduct<OP> g, TileSched sc) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    constexpr int LB = GATED_LB<OP>, BIG = gated_cols<OP>(256), HALF = gated_cols<OP>(128);
+    const int bid = blockIdx.x;
+    start_shift(bid, sc.shift);
+    int tm, tn;
+    if (bid < sc.n_big) {
+        tile_of_index(xcd_run(bid, sc.n_big), sc.tiles_m, sc.big_cols, sc.group_m, tm, tn);
+        gemm_tile_body<256, 256, 2, 4, KC, LB, false, PLAIN>(g, inside_row<256, KC>(g, tm * 256), inside_col<BIG>(g, tn * BIG), smem);
+    } else {
+        const int n_small = (int)gridDim.x - sc.n_big;
+        tile_of_index(xcd_run(bid - sc.n_big, n_small), sc.tiles_m, sc.small_cols, sc.group_m, tm, tn);
+        gemm_ring_body<256, 128, 4, 2, 3, KC, LB, false, PLAIN>(g, inside_row<256, KC>(g, tm * 256), inside_col<HALF>(g, sc.big_cols * BIG + tn * HALF), smem, threadIdx.x);
+    }
+}
+template <int OP, bool PLAIN>
+__global__ void __launch_bounds__(TILE_THREADS, 1) gated_mid_kernel(GatedProduct<OP> g, int tiles_m, int tiles_n, int group_m) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    constexpr int COLS = gated_cols<OP>(128);
+    int tm, tn;
+    tile_of_index(xcd_run(blockIdx.x, gridDim.x), tiles_m, tiles_n, group_m, tm, tn);
+    gemm_ring_body<128, 128, 4, 2, 4, KC, GATED_LB<OP>, false, PLAIN>(g, inside_row<128, KC>(g, tm * 128), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
+}
+template <int OP, bool PLAIN>
+__global__ void __launch_bounds__(TILE_THREADS, 1) gated_rect_kernel(GatedProduct<OP> g, int tiles_m, int tiles_n, int group_m) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    constexpr int COLS = gated_cols<OP>(128);
+    int tm, tn;
+    tile_of_index(xcd_run(blockIdx.x, gridDim.x), tiles_m, tiles_n, group_m, tm, tn);
+    gemm_ring_body<64, 128, 2, 4, 4, KC, GATED_LB<OP>, false, PLAIN>(g, inside_row<64, KC>(g, tm * 64), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
+}
+template <int OP, bool PLAIN>
+__global__ void __launch_bounds__(256, 2) gated_small_kernel(GatedProduct<OP> g, int tiles_m, int tiles_n, int group_m) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    constexpr int COLS = gated_cols<OP>(64);
+    int tm, tn;
+    tile_of_index(xcd_run(blockIdx.x, gridDim.x), tiles_m, tiles_n, group_m, tm, tn);
+    gemm_ring_body<64, 64, 2, 2, 4, KC, GATED_LB<OP>, false, PLAIN>(g, inside_row<64, KC>(g, tm * 64), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
 }
 
 }  // namespace axo

@@ -41,6 +41,7 @@
 #include <type_traits>
 
 #include "axo_common.hpp"
+#include "gate.hpp"
 
 namespace axo {
 
@@ -263,6 +264,18 @@ struct LineFragAddr {
     }
     __device__ __forceinline__ bf16x8 read(const char* lds0, int s, int t, int kq) const {
         return *reinterpret_cast<const bf16x8*>(lds0 + (s == D - 1 ? last[kq] : a[kq] + s * STAGE_STRIDE) + t * (16 * TILE_BK * 2));
+    }
+};
+
+// FragAddr of two operands of ROWS / 2 columns each in the place of one, [first: all stages][second: all stages] in LDS: a wave's first NT / 2
+// MFMA tiles come from the first, the others are the same columns of the second.
+template <int ROWS, int LAYOUT, int NT, int STAGES>
+struct PairFragAddr {
+    static constexpr int SECOND = STAGES * (ROWS / 2) * TILE_BK * 2;
+    FragAddr<ROWS / 2, LAYOUT, NT / 2> half;
+    __device__ __forceinline__ void init(int row0, int lane, uint32_t tile_base) { half.init(row0 / 2, lane, tile_base); }
+    __device__ __forceinline__ bf16x8 read(const char* lds0, int s, int t, int kq) const {
+        return half.read(lds0 + (t < NT / 2 ? 0 : SECOND), s, t % (NT / 2), kq);
     }
 };
 
@@ -901,13 +914,164 @@ struct SmallEpilogue {
     }
 };
 
+// ---- epilogues of a gated block ---------------------------------------------------------------
+// Eight outputs of a row, the first `valid` of them inside the matrix.
+template <bool PLAIN>
+__device__ __forceinline__ void store_eight(const u32x4 v, bf16_t* to, const bool whole, const int valid) {
+    if (whole) store_row<PLAIN>(v, reinterpret_cast<u32x4*>(to));
+    else if (valid >= 8) *reinterpret_cast<u32x4*>(to) = v;
+    else
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < valid) to[e] = (bf16_t)(v[e / 2] >> (e % 2 * 16));
+}
+
+// Forward: a wave's first TN / 2 blocks of 16 columns are those of G, the others the same columns of U, so H is formed in registers.  A
+// wave has only half of a 128-byte line of a row of H, so the whole tile is staged in LDS and stored by rows of the tile; G and U, where they are wanted,
+// go the same way in turn, through two regions.
+template <typename C, int BM, int BN, bool PLAIN, typename Args>
+__device__ __forceinline__ void gated_fwd_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int i0, const int j0, const int wm, const int wn,
+                                                   const int tid, char* smem) {
+    constexpr int COLS = BN / 2, STRIDE = COLS * 2 + 16, BYTES = BM * STRIDE, HALF = C::TN / 2;
+    constexpr int CPR = COLS / 8, ROUNDS = BM * CPR / C::THREADS;  // chunks per row, per thread
+    static_assert(2 * BYTES <= C::LDS_BYTES && BM * CPR % C::THREADS == 0, "two regions, whole rounds");
+    const int lane = tid & 63;
+    const bool whole = i0 + BM <= g.Mo && j0 + COLS <= g.No;
+    const int wcol = wn * (C::WTN / 2) + 4 * (lane >> 4), wrow = wm * C::WTM + (lane & 15);
+    if (g.bias || g.bias2) {
+#pragma unroll
+        for (int b = 0; b < HALF; ++b) {
+            const int col = j0 + wcol + b * 16, valid = min(4, g.No - col);
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            const f32x4 bg = g.bias ? load_bf16x4(g.bias + col, valid) : zero, bu = g.bias2 ? load_bf16x4(g.bias2 + col, valid) : zero;
+#pragma unroll
+            for (int a = 0; a < C::TM; ++a) {
+                acc[a][b] += bg;
+                acc[a][b + HALF] += bu;
+            }
+        }
+    }
+    __syncthreads();  // all waves are done reading the operand buffers
+    auto stage = [&](char* region, auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < HALF; ++b)
+#pragma unroll
+            for (int a = 0; a < C::TM; ++a) {
+                const f32x4 v = f(acc[a][b], acc[a][b + HALF]);
+                *reinterpret_cast<uint2*>(region + (wrow + a * 16) * STRIDE + (wcol + b * 16) * 2) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+            }
+    };
+    auto out = [&](const char* region, bf16_t* to, const int64_t ld) __attribute__((always_inline)) {
+        __syncthreads();
+        u32x4 v[ROUNDS];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {  // all reads ahead of the first store, as in tile_epilogue
+            const int q = i * C::THREADS + tid;
+            v[i] = *reinterpret_cast<const u32x4*>(region + q / CPR * STRIDE + q % CPR * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int q = i * C::THREADS + tid, row = i0 + q / CPR, col = j0 + q % CPR * 8;
+            if (whole || (row < g.Mo && col < g.No)) store_eight<PLAIN>(v[i], to + (int64_t)row * ld + col, whole, g.No - col);
+        }
+    };
+    with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
+        stage(smem, [](f32x4 x, f32x4 u) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = gate_value<decltype(gate)::value>(x[e]) * u[e];
+            return x;
+        });
+    });
+    out(smem, g.C, g.ldc);
+    if (!g.G) return;
+    stage(smem + BYTES, [](f32x4 x, f32x4) { return x; });
+    out(smem + BYTES, g.G, g.ldz);
+    stage(smem, [](f32x4, f32x4 u) { return u; });  // behind the barrier after which H has been read
+    out(smem, g.U, g.ldz);
+}
+
+// Backward: dG = sum U act'(G), dU = sum act(G).  A wave stages its sums in fp32, 16 or 32 rows at a time, so that a lane then holds eight columns of a
+// row, reads G and U and stores both results 16 bytes at a time; what a pass reads is requested a pass ahead.
+template <typename C, bool PLAIN, typename Args>
+__device__ __forceinline__ void gated_dact_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int wrow0, const int wcol0, const int wave, const int lane,
+                                                    char* smem, const bool whole) {
+    constexpr int F_STRIDE = C::WTN * 4 + 16, ROWS = C::TM * C::TN == 32 ? 16 : 32, LPR = C::WTN / 8, RPI = 64 / LPR, ITERS = ROWS / RPI, PASSES = C::WTM / ROWS;
+    static_assert(C::WAVES * ROWS * F_STRIDE <= C::LDS_BYTES && ROWS % RPI == 0, "fits the operand buffers");
+    char* const stage = smem + wave * (ROWS * F_STRIDE);
+    const int lr = lane / LPR, lc = lane % LPR * 8, col = wcol0 + lc, valid = g.No - col;
+    u32x4 gs[ITERS], us[ITERS];
+    auto request = [&](const int row0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const int row = row0 + i * RPI + lr;
+            const int64_t at = (int64_t)row * g.ldaux + col;
+            if (whole || (row < g.Mo && valid >= 8)) {
+                gs[i] = *reinterpret_cast<const u32x4*>(g.aux + at);
+                us[i] = *reinterpret_cast<const u32x4*>(g.aux2 + at);
+            } else {
+                gs[i] = us[i] = u32x4{0u, 0u, 0u, 0u};
+                if (row < g.Mo)
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < valid) {
+                            gs[i][e / 2] |= (uint32_t)g.aux[at + e] << (e % 2 * 16);
+                            us[i][e / 2] |= (uint32_t)g.aux2[at + e] << (e % 2 * 16);
+                        }
+            }
+        }
+    };
+    request(wrow0);
+    __syncthreads();  // all waves are done reading the operand buffers
+    with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            u32x4 gn[ITERS], un[ITERS];
+#pragma unroll
+            for (int i = 0; i < ITERS; ++i) {
+                gn[i] = gs[i];
+                un[i] = us[i];
+            }
+            if (p + 1 < PASSES) request(wrow0 + (p + 1) * ROWS);
+#pragma unroll
+            for (int a = 0; a < ROWS / 16; ++a)
+#pragma unroll
+                for (int b = 0; b < C::TN; ++b)
+                    *reinterpret_cast<f32x4*>(stage + (a * 16 + (lane & 15)) * F_STRIDE + (b * 16 + 4 * (lane >> 4)) * 4) = acc[p * (ROWS / 16) + a][b];
+            __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the region is private to the wave
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < ITERS; ++i) {
+                const int r = i * RPI + lr, row = wrow0 + p * ROWS + r;
+                const f32x4 lo = *reinterpret_cast<const f32x4*>(stage + r * F_STRIDE + lc * 4), hi = *reinterpret_cast<const f32x4*>(stage + r * F_STRIDE + lc * 4 + 16);
+                u32x4 dg, du;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float s0 = e < 2 ? lo[2 * e] : hi[2 * e - 4], s1 = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
+                    const float2 a0 = gate_both<decltype(gate)::value>(__uint_as_float(gn[i][e] << 16)), a1 = gate_both<decltype(gate)::value>(__uint_as_float(gn[i][e] & 0xFFFF0000u));
+                    dg[e] = pack_bf16x2(s0 * __uint_as_float(un[i][e] << 16) * a0.y, s1 * __uint_as_float(un[i][e] & 0xFFFF0000u) * a1.y);
+                    du[e] = pack_bf16x2(s0 * a0.x, s1 * a1.x);
+                }
+                if (whole || (row < g.Mo && valid > 0)) {
+                    const int64_t at = (int64_t)row * g.ldc + col;
+                    store_eight<PLAIN>(dg, g.C + at, whole, valid);
+                    store_eight<PLAIN>(du, g.U + at, whole, valid);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();  // LDS operations of a wave complete in order: the next pass may overwrite
+        }
+    });
+}
+
 // One BM x BN output tile with its top-left corner at (i0, j0), whole reduction.  LINES: the rows of A, which is KC, are
 // fetched by whole cache lines (line_phase), on three stages; with them and two of B the LDS is full, so rows of B that
 // do not start on lines still put every segment into two.  The loads of a step then touch 768 lines (dgrad) or 576 (forward) instead
 // of 1024 or 832.
-template <int BM, int BN, int WGM, int WGN, int LA, int LB, bool LINES = false, bool PLAIN = false>
-__device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, const int i0, const int j0, char* smem) {
+// Products of a gated block (Args::OP): GATED_FWD has BN / 2 columns of either B in a tile, and (i0, j0) is a corner of the output; GATED_DX walks the
+// whole steps of both products and then, where the reduction is no multiple of 64, the end of either.
+template <int BM, int BN, int WGM, int WGN, int LA, int LB, bool LINES = false, bool PLAIN = false, typename Args = GemmArgs>
+__device__ __forceinline__ void gemm_tile_body(const Args& g, const int i0, const int j0, char* smem) {
     using C = TileCfg<BM, BN, WGM, WGN>;
+    constexpr bool TWO_B = Args::OP == GATED_FWD, TWO_RUNS = Args::OP == GATED_DX;
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -927,30 +1091,41 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, const int i0, 
     // On this chip the range check covers the sum of the per-lane offset and the scalar offset
     // that carries the reduction step (measured: lowering the bound by the scalar offset at every
     // step zeroed the second half of the reduction), so one constant bound serves the whole walk.
-    const int KT = (g.R + 2 * TILE_BK - 1) / (2 * TILE_BK) * 2;
-    const bool tail = (g.R % (2 * TILE_BK)) != 0;
+    [[maybe_unused]] const int run = g.R / TILE_BK;  // whole steps of one of two products
+    const int KT = TWO_RUNS ? 2 * run + (g.R % TILE_BK != 0 ? 2 : 0) : (g.R + 2 * TILE_BK - 1) / (2 * TILE_BK) * 2;
+    const bool tail = (g.R % (TWO_RUNS ? TILE_BK : 2 * TILE_BK)) != 0;
 
     // global side: descriptor at the tile origin, per-lane offsets, scalar step
     const bf16_t* Ab = (LA == KC) ? g.A + (int64_t)i0 * g.lda : g.A + i0;
     const bf16_t* Bb = (LB == KC) ? g.B + (int64_t)j0 * g.ldb : g.B + j0;
     const uint32_t a_valid = operand_bound<LA>(g.lda, min(BM, g.Mo - i0), g.R);
-    const uint32_t b_valid = operand_bound<LB>(g.ldb, min(BN, g.No - j0), g.R);
-    const u32x4_t a_rsrc = tile_rsrc(Ab, a_valid);
-    const u32x4_t b_rsrc = tile_rsrc(Bb, b_valid);
+    constexpr int B_COLS = TWO_B ? BN / 2 : BN, B_PARTS = TWO_B ? 2 : 1;
+    const uint32_t b_valid = operand_bound<LB>(g.ldb, min(B_COLS, g.No - j0), g.R);
+    std::conditional_t<TWO_RUNS, u32x4_t, const u32x4_t> a_rsrc = tile_rsrc(Ab, a_valid);
+    std::conditional_t<TWO_RUNS, u32x4_t, const u32x4_t> b_rsrc = tile_rsrc(Bb, b_valid);
+    [[maybe_unused]] u32x4_t a_runs[2], b_runs[2];  // of either product
+    if constexpr (TWO_RUNS) {
+        a_runs[0] = a_rsrc;
+        a_runs[1] = tile_rsrc(g.A2 + (int64_t)i0 * g.lda, a_valid);
+    }
+    if constexpr (TWO_B || TWO_RUNS) {
+        b_runs[0] = b_rsrc;
+        b_runs[1] = tile_rsrc((LB == KC) ? g.B2 + (int64_t)j0 * g.ldb : g.B2 + j0, b_valid);
+    }
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_void_ptr)smem;
     const uint32_t a_step = (uint32_t)((LA == KC) ? TILE_BK * 2 : (int64_t)TILE_BK * g.lda * 2);
     const uint32_t b_step = (uint32_t)((LB == KC) ? TILE_BK * 2 : (int64_t)TILE_BK * g.ldb * 2);
-    uint32_t a_off[C::A_ROUNDS], b_off[C::B_ROUNDS];
+    uint32_t a_off[C::A_ROUNDS], b_off[C::B_ROUNDS / B_PARTS];
     uint32_t a_later[C::A_ROUNDS];
     if constexpr (LINES) line_load_offsets<C::A_ROUNDS, C::THREADS>(tid, Ab, g.lda, a_off, a_later);
     else load_offsets<BM, LA, C::A_ROUNDS, C::THREADS>(tid, g.lda, a_off);
-    load_offsets<BN, LB, C::B_ROUNDS, C::THREADS>(tid, g.ldb, b_off);
+    load_offsets<B_COLS, LB, C::B_ROUNDS / B_PARTS, C::THREADS>(tid, g.ldb, b_off);
 
     // LDS side: [A stage 0][A stage 1][B stage 0][B stage 1] (LINES: three stages of A); fragment addresses of stage 0
     static_assert(!LINES || LA == KC, "lines of rows");
     constexpr int A_STAGES = LINES ? 3 : 2;
     std::conditional_t<LINES, LineFragAddr<BM, A_STAGES>, FragAddr<BM, LA, C::TM>> fra;
-    FragAddr<BN, LB, C::TN> frb;
+    std::conditional_t<TWO_B, PairFragAddr<BN, LB, C::TN, 2>, FragAddr<BN, LB, C::TN>> frb;
     if constexpr (LINES) fra.init(wm * C::WTM, lane, 0, Ab, g.lda);
     else fra.init(wm * C::WTM, lane, 0);
     frb.init(wn * C::WTN, lane, A_STAGES * C::A_BYTES);
@@ -1011,12 +1186,28 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, const int i0, 
                 load_lds(smem_base + sa * C::A_BYTES + (j * C::THREADS + wave * 64) * 16, a_off[j], a_rsrc, a_soff);
             } else {
                 const int jb = j - C::A_ROUNDS;
+                if constexpr (TWO_B) {
+                    const int part = jb / (C::B_ROUNDS / 2), jp = jb % (C::B_ROUNDS / 2);
+                    load_lds(smem_base + A_STAGES * C::A_BYTES + (part * 2 + s) * (C::B_BYTES / 2) + (jp * C::THREADS + wave * 64) * 16,
+                             b_off[jp], b_runs[part], b_soff);
+                } else
                 load_lds(smem_base + A_STAGES * C::A_BYTES + s * C::B_BYTES + (jb * C::THREADS + wave * 64) * 16,
                          b_off[jb], b_rsrc, b_soff);
             }
         }
     };
+    [[maybe_unused]] int loading = 0;
     auto advance = [&]() __attribute__((always_inline)) {
+        if constexpr (TWO_RUNS) {  // the whole steps of the first product, those of the second, the end of the first, of the second
+            ++loading;
+            const bool second = loading < 2 * run ? loading >= run : loading > 2 * run;
+            a_rsrc[0] = second ? a_runs[1][0] : a_runs[0][0];  // the descriptors differ in nothing but their base
+            a_rsrc[1] = second ? a_runs[1][1] : a_runs[0][1];
+            b_rsrc[0] = second ? b_runs[1][0] : b_runs[0][0];
+            b_rsrc[1] = second ? b_runs[1][1] : b_runs[0][1];
+            a_soff = b_soff = (uint32_t)(loading < run ? loading : loading < 2 * run ? loading - run : run) * (TILE_BK * 2);
+            return;
+        }
         a_soff += a_step;
         b_soff += b_step;
     };
@@ -1056,7 +1247,7 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, const int i0, 
             }
         };
         auto clear_both = [&](auto part_tag) __attribute__((always_inline)) {
-            const int rem = g.R - (KT - 2 + step) * TILE_BK;
+            const int rem = TWO_RUNS ? g.R % TILE_BK : g.R - (KT - 2 + step) * TILE_BK;
             if (LINES) {  // stages KT - 2 and KT - 1 of A with step KT - 2 of B, stage KT with step KT - 1
                 if (step == 0) clear(part_tag, IC<1>{}, smem, C::A_ROUNDS, rem);
                 clear(part_tag, IC<1>{}, smem + (step + 1) * C::A_BYTES, C::A_ROUNDS, rem - TILE_BK);
@@ -1159,7 +1350,9 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, const int i0, 
     step(1, T1{}, false, false, false, false);
     AXO_SETPRIO(0);
 
-    if (i0 + BM <= g.Mo && j0 + BN <= g.No) tile_epilogue<C, LA, LB, PLAIN>(g, acc, i0, j0, wave, wm, wn, lane, smem);
+    if constexpr (Args::OP == GATED_FWD) gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
+    else if constexpr (Args::OP == GATED_DACT) gated_dact_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, i0 + BM <= g.Mo && j0 + BN <= g.No);
+    else if (i0 + BM <= g.Mo && j0 + BN <= g.No) tile_epilogue<C, LA, LB, PLAIN>(g, acc, i0, j0, wave, wm, wn, lane, smem);
     else tile_epilogue_clipped<C, LA, LB>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem);
 }
 
@@ -1181,14 +1374,16 @@ __device__ __forceinline__ void gemm_tile_body(const GemmArgs& g, const int i0, 
 // reduction 6144 on half-width ones 80.3 -> 76.2, 10600 x 7736 with reduction 48 73.4 -> 66.4.
 // `tid`: among the threads that work on the tile; `store`: false for a tile whose results are not wanted, as the second of a
 // pair of workgroup halves that has none (both halves meet at the same barriers; for tiles below 128 x 128).
-template <int BM, int BN, int WGM, int WGN, int D, int LA, int LB, bool LINES = false, bool PLAIN = false>
-__device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, const int j0, char* smem, const int tid,
+template <int BM, int BN, int WGM, int WGN, int D, int LA, int LB, bool LINES = false, bool PLAIN = false, typename Args = GemmArgs>
+__device__ __forceinline__ void gemm_ring_body(const Args& g, const int i0, const int j0, char* smem, const int tid,
                                                const bool store = true) {
     using C = RingCfg<BM, BN, WGM, WGN, D>;
+    constexpr bool TWO_B = Args::OP == GATED_FWD, TWO_RUNS = Args::OP == GATED_DX;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WGN, wn = wave % WGN;
-    const int KT = (g.R + TILE_BK - 1) / TILE_BK;
+    [[maybe_unused]] const int run = g.R / TILE_BK;  // whole steps of one of two products
+    const int KT = TWO_RUNS ? 2 * run + (g.R % TILE_BK != 0 ? 2 : 0) : (g.R + TILE_BK - 1) / TILE_BK;
     // Nothing is under way here, but the compiler does not know that: in gemm_group_kernel it lets the kinds of tiles follow each other and takes
     // what an epilogue of another kind reads for its last outputs to be pending, where those outputs are not stored.  It then waited for that
     // in the loop, s_waitcnt vmcnt(0) in every turn, which empties the ring (half-width forward tiles and pairs; the three
@@ -1201,19 +1396,30 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
 
     const bf16_t* const Ab = (LA == KC) ? g.A + (int64_t)i0 * g.lda : g.A + i0;
     const bf16_t* const Bb = (LB == KC) ? g.B + (int64_t)j0 * g.ldb : g.B + j0;
-    const u32x4_t a_rsrc = tile_rsrc(Ab, operand_bound<LA>(g.lda, min(BM, g.Mo - i0), g.R));
-    const u32x4_t b_rsrc = tile_rsrc(Bb, operand_bound<LB>(g.ldb, min(BN, g.No - j0), g.R));
+    constexpr int B_COLS = TWO_B ? BN / 2 : BN, B_PARTS = TWO_B ? 2 : 1;
+    std::conditional_t<TWO_RUNS, u32x4_t, const u32x4_t> a_rsrc = tile_rsrc(Ab, operand_bound<LA>(g.lda, min(BM, g.Mo - i0), g.R));
+    std::conditional_t<TWO_RUNS, u32x4_t, const u32x4_t> b_rsrc = tile_rsrc(Bb, operand_bound<LB>(g.ldb, min(B_COLS, g.No - j0), g.R));
+    [[maybe_unused]] u32x4_t a_runs[2], b_runs[2];  // of either product
+    if constexpr (TWO_RUNS) {
+        a_runs[0] = a_rsrc;
+        a_runs[1] = tile_rsrc(g.A2 + (int64_t)i0 * g.lda, a_rsrc[2]);
+    }
+    if constexpr (TWO_B || TWO_RUNS) {
+        b_runs[0] = b_rsrc;
+        b_runs[1] = tile_rsrc((LB == KC) ? g.B2 + (int64_t)j0 * g.ldb : g.B2 + j0, b_rsrc[2]);
+    }
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_void_ptr)smem;
     const uint32_t a_step = (uint32_t)((LA == KC) ? TILE_BK * 2 : (int64_t)TILE_BK * g.lda * 2);
     const uint32_t b_step = (uint32_t)((LB == KC) ? TILE_BK * 2 : (int64_t)TILE_BK * g.ldb * 2);
-    uint32_t a_off[C::A_ROUNDS], b_off[C::B_ROUNDS];
+    uint32_t a_off[C::A_ROUNDS], b_off[C::B_ROUNDS / B_PARTS];
     uint32_t a_later[C::A_ROUNDS], b_later[C::B_ROUNDS];
     if constexpr (A_LINES) line_load_offsets<C::A_ROUNDS, C::THREADS>(tid, Ab, g.lda, a_off, a_later);
     else load_offsets<BM, LA, C::A_ROUNDS, C::THREADS>(tid, g.lda, a_off);
     if constexpr (B_LINES) line_load_offsets<C::B_ROUNDS, C::THREADS>(tid, Bb, g.ldb, b_off, b_later);
-    else load_offsets<BN, LB, C::B_ROUNDS, C::THREADS>(tid, g.ldb, b_off);
+    else load_offsets<B_COLS, LB, C::B_ROUNDS / B_PARTS, C::THREADS>(tid, g.ldb, b_off);
     std::conditional_t<A_LINES, LineFragAddr<BM, D>, FragAddr<BM, LA, C::TM>> fra;
-    std::conditional_t<B_LINES, LineFragAddr<BN, D>, FragAddr<BN, LB, C::TN>> frb;
+    static_assert(!B_LINES || !TWO_B, "one operand by lines");
+    std::conditional_t<B_LINES, LineFragAddr<BN, D>, std::conditional_t<TWO_B, PairFragAddr<BN, LB, C::TN, D>, FragAddr<BN, LB, C::TN>>> frb;
     if constexpr (A_LINES) fra.init(wm * C::WTM, lane, 0, Ab, g.lda);
     else fra.init(wm * C::WTM, lane, 0);
     if constexpr (B_LINES) frb.init(wn * C::WTN, lane, D * C::A_BYTES, Bb, g.ldb);
@@ -1243,6 +1449,7 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
     constexpr int N_MFMA = C::TM * C::TN, RD = (LA == KC ? 1 : 2) * C::TM + (LB == KC ? 1 : 2) * C::TN;
     constexpr int NL = C::A_ROUNDS + C::B_ROUNDS;
     uint32_t a_soff = 0, b_soff = 0;
+    [[maybe_unused]] int loading = 0;
     auto load_lds = [](uint32_t lds_dst, uint32_t off, u32x4_t rsrc, uint32_t soff) __attribute__((always_inline)) {
         asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
                      :
@@ -1254,12 +1461,25 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
 #pragma unroll
         for (int j = LO; j < HI; ++j) {
             if (j < C::A_ROUNDS) load_lds(smem_base + s * C::A_BYTES + (j * C::THREADS + wave * 64) * 16, a_off[j], a_rsrc, a_soff);
-            else load_lds(smem_base + D * C::A_BYTES + s * C::B_BYTES + ((j - C::A_ROUNDS) * C::THREADS + wave * 64) * 16,
+            else if constexpr (TWO_B) {
+                const int part = (j - C::A_ROUNDS) / (C::B_ROUNDS / 2), jp = (j - C::A_ROUNDS) % (C::B_ROUNDS / 2);
+                load_lds(smem_base + D * C::A_BYTES + (part * D + s) * (C::B_BYTES / 2) + (jp * C::THREADS + wave * 64) * 16, b_off[jp], b_runs[part], b_soff);
+            } else load_lds(smem_base + D * C::A_BYTES + s * C::B_BYTES + ((j - C::A_ROUNDS) * C::THREADS + wave * 64) * 16,
                           b_off[j - C::A_ROUNDS], b_rsrc, b_soff);
         }
         if (HI == NL) {
-            a_soff += a_step;
-            b_soff += b_step;
+            if constexpr (TWO_RUNS) {  // as in gemm_tile_body
+                ++loading;
+                const bool second = loading < 2 * run ? loading >= run : loading > 2 * run;
+                a_rsrc[0] = second ? a_runs[1][0] : a_runs[0][0];
+                a_rsrc[1] = second ? a_runs[1][1] : a_runs[0][1];
+                b_rsrc[0] = second ? b_runs[1][0] : b_runs[0][0];
+                b_rsrc[1] = second ? b_runs[1][1] : b_runs[0][1];
+                a_soff = b_soff = (uint32_t)(loading < run ? loading : loading < 2 * run ? loading - run : run) * (TILE_BK * 2);
+            } else {
+                a_soff += a_step;
+                b_soff += b_step;
+            }
         }
     };
     constexpr int NH = (NL + 1) / 2;
@@ -1281,7 +1501,7 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
         AXO_SETPRIO(2);
         if (left >= D - AHEAD) issue(IC<NH>{}, IC<NL>{}, (s + D - 1) % D);
         read(s, 1);
-        if (left == 1 && (LA == KC || LB == KC) && g.R % TILE_BK != 0) {
+        if (left <= (TWO_RUNS ? 2 : 1) && (LA == KC || LB == KC) && g.R % TILE_BK != 0) {
             mask(0, g.R % TILE_BK);
             mask(1, g.R % TILE_BK);
         }
@@ -1311,8 +1531,9 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
     enum { EARLY, LATE, MIXED };
     constexpr bool SMALL = BM <= 128;
     constexpr int EPILOGUE = BM * BN < 128 * 128 || (LA == KC && LB == MC) ? EARLY : LB == KC ? MIXED : LATE;
-    [[maybe_unused]] std::conditional_t<SMALL, SmallEpilogue<C, LA, LB>, char> epilogue;
-    if constexpr (SMALL && EPILOGUE == EARLY) epilogue.request(g, i0 + wm * C::WTM, j0 + wn * C::WTN, lane);
+    constexpr bool OWN_EPILOGUE = Args::OP == GATED_FWD || Args::OP == GATED_DACT;
+    [[maybe_unused]] std::conditional_t<SMALL && !OWN_EPILOGUE, SmallEpilogue<C, LA, LB>, char> epilogue;
+    if constexpr (SMALL && EPILOGUE == EARLY && !OWN_EPILOGUE) epilogue.request(g, i0 + wm * C::WTM, j0 + wn * C::WTN, lane);
     const int lead = KT % D, first = lead > 0 ? D - lead : 0;
 #pragma unroll
     for (int i = 0; i < D; ++i) {
@@ -1362,6 +1583,9 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
     if (KT >= 2) step(IC<D - 2>{}, IC<2>{});
     step(IC<D - 1>{}, IC<1>{});
     const bool whole = i0 + BM <= g.Mo && j0 + BN <= g.No;
+    if constexpr (Args::OP == GATED_FWD) return gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
+    else if constexpr (Args::OP == GATED_DACT) return gated_dact_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, whole);
+    else {
     if constexpr (!SMALL || EPILOGUE == MIXED)
         if (whole) return tile_epilogue<C, LA, LB, PLAIN>(g, acc, i0, j0, wave, wm, wn, lane, smem);
     if constexpr (SMALL) {
@@ -1369,6 +1593,7 @@ __device__ __forceinline__ void gemm_ring_body(const GemmArgs& g, const int i0, 
         __syncthreads();  // all waves are done reading the operand buffers; outside the branch, which the halves of a pair take differently
         if (store) epilogue.finish(g, acc, wave, smem, whole);
     } else tile_epilogue_clipped<C, LA, LB>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem);
+    }
 }
 
 using MixBigCfg = TileCfg<256, 256, 2, 4>;

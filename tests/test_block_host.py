@@ -181,7 +181,7 @@ def test_nothing_to_do(name):
     nothing = {k: None for k, v in GOOD[name].items() if isinstance(v, int) and v >= at(1) and k != "ws_bytes"}
     lds = {k: 0 for k in GOOD[name] if k.startswith("ld")}
     if name == "axo_gated_wgrad" or name == "axo_gated_wgrad_acc":
-        assert call(name, p=P(T=64, K=0), **nothing, **lds) == 0
+        assert call(name, p=P(T=64, K=0), **{**nothing, "dG": at(2), "dU": at(3)}, **{**lds, "lddz": 48}) == 0
         assert call(name, p=P(T=64, N=0), **{**nothing, "X": at(1)}, **{**lds, "ldx": 32}) == 0
     else:  # weights have elements without tokens, too
         weights = {k: GOOD[name][k] for k in ("Wg", "Wu", "W", "ldw") if k in GOOD[name]}
