@@ -62,42 +62,81 @@ bool valid_eps(float eps) { return eps >= 0.0f && std::isfinite(eps); }
 // A workgroup to a row; more rows than this are walked.
 constexpr int64_t NORM_MOST_BLOCKS = 1 << 20;
 
-int launch_norm(const axo::NormArgs& g, int type, hipStream_t st) {
-    if (g.M == 0 || g.K == 0) return AXO_OK;
-    const dim3 grid(at_most(g.M, NORM_MOST_BLOCKS)), block(axo::NORM_THREADS);
-    if (type == AXO_TYPE_F32) hipLaunchKernelGGL(axo::norm_long_kernel<float>, grid, block, 0, st, g);
-    else hipLaunchKernelGGL(axo::norm_long_kernel<bf16_t>, grid, block, 0, st, g);
+template <typename T, int LANES, int CH>
+int launch_norm_rows(const axo::NormArgs& g, hipStream_t st) {
+    constexpr int BLOCK = LANES <= 64 ? 256 : LANES, ROWS = BLOCK / LANES;
+    hipLaunchKernelGGL((axo::norm_rows_kernel<T, LANES, CH>), dim3(at_most(tiles_in(g.M, ROWS), NORM_MOST_BLOCKS)), dim3(BLOCK), 0, st, g);
     return launched();
 }
-
-// Row slices of the column sums.
-struct NormSlices {
-    int slices, rows;
-};
-NormSlices norm_slices(int64_t M) {
-    const int64_t rows = std::max<int64_t>(axo::NORM_COL_ROWS, (M + 255) / 256);
-    return {(int)std::max<int64_t>(1, (M + rows - 1) / rows), (int)rows};
+template <typename T>
+int launch_norm_typed(const axo::NormArgs& g, hipStream_t st) {
+    if (g.K <= 64) return launch_norm_rows<T, 8, 1>(g, st);
+    if (g.K <= 128) return launch_norm_rows<T, 16, 1>(g, st);
+    if (g.K <= 256) return launch_norm_rows<T, 32, 1>(g, st);
+    if (g.K <= 512) return launch_norm_rows<T, 64, 1>(g, st);
+    if (g.K <= 1024) return launch_norm_rows<T, 64, 2>(g, st);
+    if (g.K <= 2048) return launch_norm_rows<T, 256, 1>(g, st);
+    if (g.K <= 4096) return launch_norm_rows<T, 256, 2>(g, st);
+    if (g.K <= 8192) return launch_norm_rows<T, 256, 4>(g, st);
+    if (g.K <= 12288) return launch_norm_rows<T, 512, 3>(g, st);
+    if (g.K <= 16384) return launch_norm_rows<T, 512, 4>(g, st);
+    if (g.K <= 32768) return launch_norm_rows<T, 1024, 4>(g, st);
+    hipLaunchKernelGGL(axo::norm_long_kernel<T>, dim3(at_most(g.M, NORM_MOST_BLOCKS)), dim3(axo::NORM_THREADS), 0, st, g);
+    return launched();
 }
-size_t norm_workspace(int64_t M, int64_t K) { return (size_t)norm_slices(M).slices * 2 * (size_t)K * sizeof(float); }
+int launch_norm(const axo::NormArgs& g, int type, hipStream_t st) {
+    if (g.M == 0 || g.K == 0) return AXO_OK;
+    return type == AXO_TYPE_F32 ? launch_norm_typed<float>(g, st) : launch_norm_typed<bf16_t>(g, st);
+}
 
-int launch_norm_bwd(axo::NormBwdArgs g, int type, hipStream_t st) {
-    if (g.K == 0) return AXO_OK;
+// The column sums of the backward pass come from so many workgroups at most, each of which leaves 2 K of them in the workspace.
+constexpr int NORM_MOST_SLICES = 256;
+constexpr int NORM_MOST_COLS = 16384;  // of rows in registers
+int norm_slice_rows(int64_t M) { return (int)std::max<int64_t>(axo::NORM_COL_ROWS, (M + 255) / 256); }  // of longer ones
+size_t norm_workspace(int64_t M, int64_t K) {
+    return (size_t)std::max<int64_t>(1, std::min<int64_t>(M, NORM_MOST_SLICES)) * 2 * (size_t)K * sizeof(float);
+}
+
+int launch_norm_join(const axo::NormBwdArgs& g, hipStream_t st) {
+    if (g.phase == axo::NORM_APPLY || (!g.dgamma && !g.dbeta)) return AXO_OK;
+    hipLaunchKernelGGL(axo::norm_join_kernel, dim3((unsigned)((2 * (int64_t)g.K + axo::NORM_JOIN_COLS - 1) / axo::NORM_JOIN_COLS)), dim3(axo::NORM_JOIN_THREADS), 0, st, g);
+    return launched();
+}
+template <typename T, int LANES, int CH, int GROUPS>
+int launch_norm_bwd_rows(axo::NormBwdArgs& g, hipStream_t st) {
+    g.slices = (int)std::min<int64_t>(tiles_in(g.M, GROUPS), NORM_MOST_SLICES);
+    hipLaunchKernelGGL((axo::norm_bwd_rows_kernel<T, LANES, CH, GROUPS>), dim3((unsigned)g.slices), dim3(LANES * GROUPS), 0, st, g);
+    if (const int rc = launched()) return rc;
+    return launch_norm_join(g, st);
+}
+template <typename T>
+int launch_norm_bwd_typed(axo::NormBwdArgs& g, hipStream_t st) {
+    if (g.M > 0 && g.K <= NORM_MOST_COLS) {
+        if (g.K <= 64) return launch_norm_bwd_rows<T, 8, 1, 32>(g, st);
+        if (g.K <= 128) return launch_norm_bwd_rows<T, 16, 1, 32>(g, st);
+        if (g.K <= 256) return launch_norm_bwd_rows<T, 32, 1, 16>(g, st);
+        if (g.K <= 512) return launch_norm_bwd_rows<T, 64, 1, 8>(g, st);
+        if (g.K <= 1024) return launch_norm_bwd_rows<T, 128, 1, 8>(g, st);
+        if (g.K <= 2048) return launch_norm_bwd_rows<T, 256, 1, 4>(g, st);
+        if (g.K <= 4096) return launch_norm_bwd_rows<T, 512, 1, 2>(g, st);
+        if (g.K <= 8192) return launch_norm_bwd_rows<T, 512, 2, 1>(g, st);
+        if (g.K <= 12288) return launch_norm_bwd_rows<T, 512, 3, 1>(g, st);
+        return launch_norm_bwd_rows<T, 1024, 2, 1>(g, st);
+    }
     if (g.M > 0) {
-        const dim3 grid(at_most(g.M, NORM_MOST_BLOCKS)), block(axo::NORM_THREADS);
-        if (type == AXO_TYPE_F32) hipLaunchKernelGGL(axo::norm_bwd_long_kernel<float>, grid, block, 0, st, g);
-        else hipLaunchKernelGGL(axo::norm_bwd_long_kernel<bf16_t>, grid, block, 0, st, g);
+        hipLaunchKernelGGL(axo::norm_bwd_long_kernel<T>, dim3(at_most(g.M, NORM_MOST_BLOCKS)), dim3(axo::NORM_THREADS), 0, st, g);
         if (const int rc = launched()) return rc;
     }
     if (g.phase == axo::NORM_APPLY || (!g.dgamma && !g.dbeta)) return AXO_OK;
-    const NormSlices s = norm_slices(g.M);
-    g.slices = s.slices;
-    g.rows_per_slice = s.rows;
-    const dim3 grid((unsigned)(tiles_in(g.K, axo::NORM_STRIP) * s.slices)), block(axo::NORM_COL_THREADS);
-    if (type == AXO_TYPE_F32) hipLaunchKernelGGL(axo::norm_cols_kernel<float>, grid, block, 0, st, g);
-    else hipLaunchKernelGGL(axo::norm_cols_kernel<bf16_t>, grid, block, 0, st, g);
+    g.rows_per_slice = norm_slice_rows(g.M);
+    g.slices = (int)std::max<int64_t>(1, tiles_in(g.M, g.rows_per_slice));
+    hipLaunchKernelGGL(axo::norm_cols_kernel<T>, dim3((unsigned)(tiles_in(g.K, axo::NORM_STRIP) * g.slices)), dim3(axo::NORM_COL_THREADS), 0, st, g);
     if (const int rc = launched()) return rc;
-    hipLaunchKernelGGL(axo::norm_join_kernel, dim3((unsigned)((2 * (int64_t)g.K + 255) / 256)), dim3(256), 0, st, g);
-    return launched();
+    return launch_norm_join(g, st);
+}
+int launch_norm_bwd(axo::NormBwdArgs g, int type, hipStream_t st) {
+    if (g.K == 0) return AXO_OK;
+    return type == AXO_TYPE_F32 ? launch_norm_bwd_typed<float>(g, st) : launch_norm_bwd_typed<bf16_t>(g, st);
 }
 
 int plan_norm(const axo_problem_t* p, const void* X, int64_t ldx, const void* R, int64_t ldr, int type, void* S, int64_t lds, Buffers& b,

@@ -4,6 +4,8 @@
 //             dgamma = sum over rows of dy h, dbeta = sum over rows of dy
 // All of it moves each element once or twice and computes some ten operations on it: bound by memory.
 #pragma once
+#include <type_traits>
+
 #include "axo_common.hpp"
 
 namespace axo {
@@ -95,13 +97,28 @@ __device__ __forceinline__ void store_chunk(float* p, int valid, const float (&v
 __device__ __forceinline__ float stored(float v, const float*) { return v; }
 __device__ __forceinline__ float stored(float v, const bf16_t*) { return __uint_as_float(pack_bf16x2(v, 0.f) << 16); }
 
+// The sum of a value over groups of LANES lanes, the same in all lanes of a group: inside 16 lanes by the exchanges that an addition takes along, between them through
+// the LDS crossbar.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+    auto with = [](float x, auto ctrl) __attribute__((always_inline)) {
+        return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    if constexpr (LANES >= 2) v = with(v, std::integral_constant<int, 0xB1>{});    // quad: 1 0 3 2
+    if constexpr (LANES >= 4) v = with(v, std::integral_constant<int, 0x4E>{});    // quad: 2 3 0 1
+    if constexpr (LANES >= 8) v = with(v, std::integral_constant<int, 0x141>{});   // mirrored halves of 16
+    if constexpr (LANES >= 16) v = with(v, std::integral_constant<int, 0x140>{});  // mirrored 16
+    const int lane = threadIdx.x & 63;
+    if constexpr (LANES >= 32) v += __int_as_float(__builtin_amdgcn_ds_bpermute((lane ^ 16) * 4, __float_as_int(v)));
+    if constexpr (LANES >= 64) v += __int_as_float(__builtin_amdgcn_ds_bpermute((lane ^ 32) * 4, __float_as_int(v)));
+    return v;
+}
+
 // Sums of a workgroup's values, the same in every thread and in a fixed order; `lds`: a float per wave and value.
 template <int THREADS, int N>
 __device__ __forceinline__ void block_sums(float (&v)[N], float* lds) {
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1)
-#pragma unroll
-        for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], m, 64);
+    for (int n = 0; n < N; ++n) v[n] = lanes_sum<64>(v[n]);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 0)
 #pragma unroll
@@ -128,6 +145,223 @@ __device__ __forceinline__ void join_parts(const NormArgs& g, int row, float& me
         m2 += q.y + (q.x - mean) * (q.x - mean) * (float)g.K;
     }
     rstd = 1.0f / sqrtf(m2 / ((float)g.K * (float)g.n_parts) + g.eps);
+}
+
+// ---- rows that fit the registers of the lanes that share them -----------------------------------
+// LANES lanes hold a row, chunk j * LANES + lane of eight values in the lane's j-th of CH chunks, so that lanes beside each other load 16 bytes beside
+// each other.  Up to 64 lanes are a part of a wave or a wave, which needs no barrier; more are whole waves of a workgroup.
+template <typename T>
+struct RawChunk;
+template <>
+struct RawChunk<bf16_t> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
+    __device__ __forceinline__ float at(int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
+    __device__ __forceinline__ void keep(int n) {  // the first n values, zeros behind them
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] &= n >= 2 * i + 2 ? 0xFFFFFFFFu : n == 2 * i + 1 ? 0xFFFFu : 0u;
+    }
+};
+template <>
+struct RawChunk<float> {
+    f32x4 lo, hi;
+    __device__ __forceinline__ void load(const float* p) {
+        lo = *reinterpret_cast<const f32x4*>(p);
+        hi = *reinterpret_cast<const f32x4*>(p + 4);
+    }
+    __device__ __forceinline__ float at(int i) const { return i < 4 ? lo[i % 4] : hi[i % 4]; }
+    __device__ __forceinline__ void keep(int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo[i] = n > i ? lo[i] : 0.f;
+            hi[i] = n > i + 4 ? hi[i] : 0.f;
+        }
+    }
+};
+// What was loaded is taken to be something new from here on: nothing that was formed of it earlier is kept.
+__device__ __forceinline__ void pin_chunk(RawChunk<bf16_t>& r) { asm volatile("" : "+v"(r.w)); }
+__device__ __forceinline__ void pin_chunk(RawChunk<float>& r) { asm volatile("" : "+v"(r.lo), "+v"(r.hi)); }
+// One row that a whole wave works on: a buffer descriptor that ends with it, so that what lies behind the row's end reads as zero and is not written, and lanes need
+// no more than the offset of their chunk.  The range check works in dwords: of an odd number of bf16 values the one behind the last is
+// read and has to be masked, and the last one is stored on its own.
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const T* row, int n) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(row), 0, (int)((n * sizeof(T) + 3) & ~(size_t)3), 0x00020000);
+}
+__device__ __forceinline__ void load_from(__amdgpu_buffer_rsrc_t b, int c, RawChunk<bf16_t>& r) {
+    r.w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, c * 2, 0, 0));
+}
+__device__ __forceinline__ void load_from(__amdgpu_buffer_rsrc_t b, int c, RawChunk<float>& r) {
+    r.lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(b, c * 4, 0, 0));
+    r.hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(b, c * 4 + 16, 0, 0));
+}
+
+// A lane's chunks of a row.  Where lanes of a wave have different rows a chunk that lies behind its row's end is the first one in its place, and a chunk that the row ends in
+// reads on into the row's padding; only the last row may have none (`last`): its last chunk is fetched value by value.  mask() puts zeros in the
+// place of what is not the row's.
+template <typename T, int LANES, int CH>
+struct RowChunks {
+    RawChunk<T> raw[CH];
+    __device__ __forceinline__ void load(const T* row, int K, int lane, bool last) {
+        if constexpr (LANES >= 64) {
+            const __amdgpu_buffer_rsrc_t b = row_buffer(row, K);
+#pragma unroll
+            for (int j = 0; j < CH; ++j) load_from(b, (j * LANES + lane) * 8, raw[j]);
+        } else {
+            static_assert(CH == 1, "short rows");
+            const int c = lane * 8;
+            const bool whole = c + 8 <= K || (c < K && !last);
+            if (whole || K >= 8) raw[0].load(row + (whole ? c : 0));
+            else raw[0] = RawChunk<T>{};
+            if (c < K && !whole) {
+                float v[8];
+                load_chunk(row + c, K - c, v);
+                set(raw[0], v);
+            }
+        }
+    }
+    static __device__ __forceinline__ void set(RawChunk<bf16_t>& r, const float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = __float_as_uint(v[2 * i]) >> 16 | (__float_as_uint(v[2 * i + 1]) & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ void set(RawChunk<float>& r, const float (&v)[8]) {
+        r.lo = f32x4{v[0], v[1], v[2], v[3]};
+        r.hi = f32x4{v[4], v[5], v[6], v[7]};
+    }
+    __device__ __forceinline__ void mask(int K, int lane) {
+        if (LANES >= 64 && (sizeof(T) == 4 || K % 2 == 0)) return;
+        asm volatile("" : "+v"(lane));  // in a loop over rows the masks would be kept, four registers a chunk
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int left = K - (j * LANES + lane) * 8;
+            if (left < 8) raw[j].keep(left);
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) raw[j] = RawChunk<T>{};
+    }
+};
+// Eight values of chunk c of a row.
+template <int LANES, typename T>
+__device__ __forceinline__ void store_in_row(T* row, int K, int c, const float (&v)[8]) {
+    if constexpr (LANES < 64) {
+        if (c < K) store_chunk(row + c, K - c, v);
+    } else if constexpr (sizeof(T) == 4) {
+        const __amdgpu_buffer_rsrc_t b = row_buffer(row, K);
+        const f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), b, c * 4, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), b, c * 4 + 16, 0, 0);
+    } else {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        __builtin_amdgcn_raw_buffer_store_b128(w, row_buffer(row, K & ~1), c * 2, 0, 0);
+        if (K % 2 != 0 && c < K && c + 8 > K) {
+            const int d = (K - 1 - c) / 2;
+            row[K - 1] = (bf16_t)(d == 0 ? w[0] : d == 1 ? w[1] : d == 2 ? w[2] : w[3]);
+        }
+    }
+}
+// Sums over the LANES lanes of a row, the same in all of them.  `lds`: N floats per wave, used by rows of several waves; a caller that comes back without a
+// barrier in between alternates between two of them.
+template <int LANES, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* lds) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[n]);
+    if constexpr (LANES > 64) {
+        constexpr int WAVES = LANES / 64;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
+        if (lane == 0)
+#pragma unroll
+            for (int n = 0; n < N; ++n) lds[wave * N + n] = v[n];
+        __syncthreads();
+        constexpr int SPAN = WAVES <= 2 ? 2 : WAVES <= 4 ? 4 : WAVES <= 8 ? 8 : 16;
+        static_assert(WAVES <= SPAN, "waves of a workgroup");
+        const int w = lane % SPAN;
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = w < WAVES ? lds[(first + w) * N + n] : 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = lanes_sum<SPAN>(v[n]);
+    }
+}
+
+// Which of a workgroup's rows a thread works on; the compiler is told where that is the same for a whole wave, and addresses rows by scalars then.
+template <int LANES>
+__device__ __forceinline__ int row_group() {
+    return LANES < 64 ? (int)threadIdx.x / LANES : __builtin_amdgcn_readfirstlane((int)threadIdx.x / LANES);
+}
+
+template <typename T, int LANES, int CH>
+__global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES) norm_rows_kernel(NormArgs g) {
+    constexpr int BLOCK = LANES <= 64 ? 256 : LANES, ROWS = BLOCK / LANES;
+    static_assert(LANES <= 64 || ROWS == 1, "rows of several waves meet at barriers");
+    __shared__ float lds[2][BLOCK / 64];
+    const int lane = threadIdx.x % LANES;
+    // (the descriptors of rows are scalars: a row is the same for a whole wave where LANES >= 64)
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + row_group<LANES>(); row < g.M; row += (int64_t)gridDim.x * ROWS) {
+        const bool last = row == g.M - 1;
+        RowChunks<T, LANES, CH> x, r;
+        x.load(static_cast<const T*>(g.X) + row * g.ldx, g.K, lane, last);
+        if (g.R) r.load(static_cast<const T*>(g.R) + row * g.ldr, g.K, lane, last);
+        RowChunks<bf16_t, LANES, CH> gamma, beta;  // the same for all rows, from the caches
+        if (g.gamma) gamma.load(g.gamma, g.K, lane, true);
+        if (g.beta) beta.load(g.beta, g.K, lane, true);
+        x.mask(g.K, lane);
+        if (g.R) r.mask(g.K, lane);
+        float v[CH][8];
+        float sum[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = x.raw[j].at(i);
+            if (g.R) {
+                float s[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    s[i] = v[j][i] + r.raw[j].at(i);
+                    v[j][i] = stored(s[i], static_cast<const T*>(nullptr));
+                }
+                store_in_row<LANES>(static_cast<T*>(g.S) + row * g.lds, g.K, (j * LANES + lane) * 8, s);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] += v[j][i];
+        }
+        float mean, rstd;
+        if (g.phase == NORM_APPLY) join_parts(g, (int)row, mean, rstd);
+        else {
+            row_sums<LANES>(sum, lds[0]);
+            mean = sum[0] / (float)g.K;
+            sum[0] = 0.f;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int left = g.K - (j * LANES + lane) * 8;
+                if (left >= 8)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[0] += (v[j][i] - mean) * (v[j][i] - mean);
+                else
+#pragma unroll
+                    for (int i = 0; i < 7; ++i) sum[0] += i < left ? (v[j][i] - mean) * (v[j][i] - mean) : 0.f;
+            }
+            row_sums<LANES>(sum, lds[1]);
+            if (g.phase == NORM_PART) {
+                if (lane == 0) g.part[row] = float2{mean, sum[0]};
+                continue;
+            }
+            rstd = 1.0f / sqrtf(sum[0] / (float)g.K + g.eps);
+        }
+        if (lane == 0 && g.stats) g.stats[row] = float2{mean, rstd};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[j][i] = (v[j][i] - mean) * rstd;
+                if (g.gamma) v[j][i] *= gamma.raw[j].at(i);
+                if (g.beta) v[j][i] += beta.raw[j].at(i);
+            }
+            store_in_row<LANES>(g.Y + row * g.ldy, g.K, (j * LANES + lane) * 8, v[j]);
+        }
+    }
 }
 
 // Rows of any length, a workgroup to a row, which it reads once for the mean, once for the deviations and once for the output.
@@ -197,6 +431,127 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_long_kernel(NormArgs g) {
             store_chunk(g.Y + row * g.ldy + c, valid, v);
         }
     }
+}
+
+// Backward on rows in registers, one pass over the data: a workgroup of GROUPS rows at a time walks the rows, every lane keeps the sums of its columns of dgamma and
+// dbeta as it goes, and the next row's loads are under way while this row's sums meet.  At its end a workgroup adds its groups' columns up through
+// LDS, in order, and writes them to `partial`, which norm_join_kernel adds up.
+template <typename T, int LANES, int CH, int GROUPS>
+__global__ void __launch_bounds__(LANES * GROUPS) norm_bwd_rows_kernel(NormBwdArgs g) {
+    constexpr int BLOCK = LANES * GROUPS;
+    constexpr bool AHEAD = sizeof(T) == 2 || LANES * CH < 2048;  // 16 fp32 values per lane of a full workgroup leave no registers for the next row's
+    __shared__ float lds[2][2 * (BLOCK / 64)];
+    __shared__ float cols[GROUPS > 1 ? BLOCK * 8 : 1];
+    const int lane = threadIdx.x % LANES, group = row_group<LANES>();
+    const bool want_cols = g.phase != NORM_APPLY && (g.dgamma || g.dbeta), want_sums = g.phase != NORM_APPLY;
+    float dg[CH][8], db[CH][8];
+    RowChunks<bf16_t, LANES, CH> gm;
+    if (g.gamma) {
+        gm.load(g.gamma, g.K, lane, true);
+        gm.mask(g.K, lane);
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[j][i] = db[j][i] = 0.f;
+        if (!g.gamma) gm.raw[j].w = u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};  // ones
+    }
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    RowChunks<T, LANES, CH> x;
+    RowChunks<bf16_t, LANES, CH> dy;
+    float2 st;
+    auto request = [&](int64_t row) __attribute__((always_inline)) {  // rows beyond the last stand for it
+        row = min(row, (int64_t)g.M - 1);
+        const bool last = row == g.M - 1;
+        st = g.stats[row];
+        x.load(static_cast<const T*>(g.S) + row * g.lds, g.K, lane, last);
+        dy.load(g.dY + row * g.lddy, g.K, lane, last);
+    };
+    request((int64_t)blockIdx.x * GROUPS + group);
+    int turn = 0;
+    for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < g.M; row0 += step, turn ^= 1) {  // as many turns for every group
+        const int64_t row = row0 + group;
+        const bool here = row < g.M;
+        if (!AHEAD && row0 >= step) request(row);
+        RowChunks<T, LANES, CH> xs = x;
+        RowChunks<bf16_t, LANES, CH> ys = dy;
+        const float2 stats = st;
+        auto h_of = [&](int j, int i) __attribute__((always_inline)) { return (xs.raw[j].at(i) - stats.x) * stats.y; };
+        xs.mask(g.K, lane);
+        ys.mask(g.K, lane);  // with dY zero there, a row or a column that is not there adds nothing
+        if (!here) ys.clear();
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < CH; ++j) pin_chunk(gm.raw[j]);  // kept as it is loaded, not as eight registers of fp32
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = ys.raw[j].at(i), h = h_of(j, i), d = y * gm.raw[j].at(i);
+                dg[j][i] += y * h;
+                db[j][i] += y;
+                asm volatile("" : "+v"(dg[j][i]), "+v"(db[j][i]));  // here: put off, they would keep h and y in registers
+                sum[0] += d;
+                sum[1] += d * h;
+            }
+        }
+        RowChunks<T, LANES, CH> r;
+        if (g.R) r.load(static_cast<const T*>(g.R) + min(row, (int64_t)g.M - 1) * g.ldr, g.K, lane, row >= g.M - 1);
+        if (AHEAD && row0 + step < g.M) request(row + step);
+        if (want_sums) row_sums<LANES>(sum, lds[turn]);
+        if (!here) continue;
+        if (g.phase == NORM_PART) {
+            if (lane == 0) g.sums[row] = float2{sum[0], sum[1]};
+            continue;
+        }
+        if (g.phase == NORM_APPLY) {
+            sum[0] = g.sums[row].x;
+            sum[1] = g.sums[row].y;
+        }
+        const float c1 = sum[0] * g.per_row, c2 = sum[1] * g.per_row;
+        // h and dy gamma are formed again from what was loaded: kept in fp32 they would be twice to four times the registers
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            pin_chunk(xs.raw[j]);
+            pin_chunk(ys.raw[j]);
+            pin_chunk(gm.raw[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[i] = stats.y * (ys.raw[j].at(i) * gm.raw[j].at(i) - c1 - h_of(j, i) * c2);
+                if (g.R) d[i] += r.raw[j].at(i);
+            }
+            store_in_row<LANES>(static_cast<T*>(g.dX) + row * g.lddx, g.K, (j * LANES + lane) * 8, d);
+        }
+    }
+    if (!want_cols) return;
+#pragma unroll
+    for (int what = 0; what < 2; ++what)
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = what ? db[j][i] : dg[j][i];
+            if constexpr (GROUPS > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) cols[threadIdx.x * 8 + i] = v[i];
+                __syncthreads();
+                if (group == 0)
+#pragma nounroll
+                    for (int q = 1; q < GROUPS; ++q)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] += cols[(q * LANES + lane) * 8 + i];
+            }
+            const int c = (j * LANES + lane) * 8;
+            if (group == 0)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < g.K) g.partial[((int64_t)blockIdx.x * 2 + what) * g.K + c + i] = v[i];
+        }
 }
 
 // dX of rows of any length, a workgroup to a row, which it reads once for the two sums and once for the output.
@@ -309,13 +664,32 @@ __global__ void __launch_bounds__(NORM_COL_THREADS) norm_cols_kernel(NormBwdArgs
     const int64_t at = (int64_t)strip * NORM_STRIP + c;
     if (at < g.K) g.partial[((int64_t)slice * 2 + what) * g.K + at] = sum;
 }
-__global__ void __launch_bounds__(256) norm_join_kernel(NormBwdArgs g) {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= 2 * (int64_t)g.K) return;
+// 64 columns by 16 slices at a time.
+constexpr int NORM_JOIN_THREADS = 1024, NORM_JOIN_COLS = 64;
+__global__ void __launch_bounds__(NORM_JOIN_THREADS) norm_join_kernel(NormBwdArgs g) {
+    constexpr int LANES = NORM_JOIN_THREADS / NORM_JOIN_COLS;
+    __shared__ float lds[LANES][NORM_JOIN_COLS];
+    const int col = threadIdx.x % NORM_JOIN_COLS, first = threadIdx.x / NORM_JOIN_COLS;
+    const int64_t at = (int64_t)blockIdx.x * NORM_JOIN_COLS + col;  // of dgamma and dbeta behind each other
+    float sum = 0.f;
+    if (at < 2 * (int64_t)g.K) {
+        const float* const p = g.partial + at;
+        int s = first;
+        for (; s + 7 * LANES < g.slices; s += 8 * LANES) {  // eight loads in flight, added in order
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)(s + i * LANES) * 2 * g.K];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; s < g.slices; s += LANES) sum += p[(int64_t)s * 2 * g.K];
+    }
+    lds[first][col] = sum;
+    __syncthreads();
+    if (first != 0 || at >= 2 * (int64_t)g.K) return;
     float* const out = at < g.K ? g.dgamma : g.dbeta;
     if (!out) return;
-    float sum = 0.f;
-    for (int s = 0; s < g.slices; ++s) sum += g.partial[(int64_t)s * 2 * g.K + at];
+    for (int q = 1; q < LANES; ++q) sum += lds[q][col];
     const int64_t c = at < g.K ? at : at - g.K;
     out[c] = g.accumulate ? out[c] + sum : sum;
 }
