@@ -1280,6 +1280,15 @@ int launch_products(const GemmArgs* products, int n, int la, int lb, hipStream_t
 
 Tiles quickest_tiles(int Mo, int No, int R) { return tiles_of(Mo, No, R); }
 
+double tiles_time(Tiles tiles, int Mo, int No, int R) {
+    switch (tiles) {
+        case Tiles::small: return small_time(Mo, No, R) + small_time_long(Mo, No, R);
+        case Tiles::mid: return mid_time(Mo, No, R);
+        case Tiles::big: return tile_time(Mo, No, R);
+        default: return 3.5 + steps_in(R) * 0.3;
+    }
+}
+
 axo::TileSched plan_columns(int Mo, int No, int R) {
     axo::TileSched sc = plan_tiles(Mo, No);
     sc.shift = shift_units(Mo, No, R);

@@ -7,6 +7,7 @@
 
 #include "axo_host.hpp"
 #include "gated.hpp"
+#include "gated_slim.hpp"
 #include "norm.hpp"
 
 namespace axo_block {
@@ -271,19 +272,141 @@ int launch_gated_on(const GatedArgs& g, Tiles tiles, int cols, int steps, hipStr
     hipLaunchKernelGGL(kern, dim3(sc.n_big + sc.tiles_m * sc.small_cols), dim3(axo::TILE_THREADS), axo::MIX_LDS_BYTES, st, axo::GatedProduct<OP>{g}, sc);
     return launched();
 }
+// ---- split reductions (gated_slim.hpp) ----
+// The workspace: arrival counters of at most so many tiles, and behind them the sums of the slices.
+constexpr size_t GATED_COUNTER_BYTES = 8192;
+constexpr int64_t GATED_MOST_WORKGROUPS = 1400;  // of a launch whose tiles are sliced
+
+// A kind of split-reduction tile, and what a product on it takes in us: `fixed`, and the longest of
+//   - a CU's share of the workgroups, each of which takes in its operands at `rate` KB per us and costs `each` besides;
+//   - one wave's chain of chunks, `latency` each, as many under way as it has stages;
+//   - the weights, read at `tbs` TB/s;
+// and where its reduction is sliced `join` and `per_slice` for each slice.  Fitted to 100 000 measured launches of 14 000 shapes (1 to 800 tokens, widths of 32 to
+// 16384, weights from memory) with 1 to 16 slices; half of the estimates are within 8 to 17 %, nine of ten within 45 %.
+struct GatedSlim {
+    int rows, cols, waves, stages;  // `cols`: of the output
+    double fixed, rate, latency, tbs, join, per_slice, each;
+};
+constexpr GatedSlim GATED_SLIM[3][3] = {
+    {{16, 32, 4, 3, 2.0, 53.9, 2.60, 3.25, 0.57, 0.43, 2.22}, {32, 32, 4, 3, 2.0, 51.3, 2.97, 2.66, 0.83, 0.70, 2.36}, {16, 128, 2, 2, 2.0, 67.1, 1.97, 4.70, 2.35, 0.97, 4.01}},
+    {{16, 32, 4, 3, 3.06, 94.1, 0.85, 5.59, 0.68, 0.20, 1.18}, {32, 32, 4, 3, 2.0, 84.0, 1.31, 4.26, 0.44, 0.36, 2.72}, {}},
+    {{16, 32, 4, 3, 2.75, 84.6, 0.31, 4.96, 0.81, 0.18, 0.84}, {32, 32, 4, 3, 2.0, 78.3, 1.37, 3.69, 0.38, 0.36, 2.19}, {}}};
+// The same for the tiles of gemm_tile.hpp: what their estimates have to be multiplied with for these products (small, wide, tall, mid, big; medians of the same
+// shapes), which read weights from memory and have longer epilogues.  They are taken unless a split reduction is estimated at least a tenth quicker:
+// over those shapes the choice is 1.35 (forward), 1.56 and 1.91 times quicker than these tiles throughout, 4 to 7 % slower than the best of all, and by more than 5 % slower
+// than these tiles for one or two shapes in a hundred.
+constexpr double GATED_TILES[3][5] = {{1.06, 1.66, 1.66, 1.21, 1.03}, {0.93, 1.37, 1.37, 1.41, 1.55}, {0.88, 1.47, 1.47, 1.21, 1.08}};
+
+// How a product is cut into split-reduction tiles.
+struct GatedCut {
+    int kind = -1;  // of GATED_SLIM[OP], or -1: not at all
+    int64_t tiles_m = 0, tiles_n = 0;
+    int slices = 1, chunks = 0;
+    size_t bytes = 0;  // of workspace
+};
+// The quickest cut of a product (Mo x No, reductions of R) and the estimate of it.
 template <int OP>
-int launch_gated(const GatedArgs& g, hipStream_t st) {
-    if (g.Mo == 0 || g.No == 0) return AXO_OK;
-    // as one product: twice the columns, or twice the reduction
-    const int64_t cols = OP == axo::GATED_FWD ? 2 * (int64_t)g.No : g.No, red = OP == axo::GATED_DX ? 2 * (int64_t)g.R : g.R;
-    if (g.R == 0 || !gated_spans_ok<OP>(g) || cols > INT32_MAX || red > INT32_MAX || !grid_fits(tiles_in(g.Mo, 64) * tiles_in((int)cols, 64), axo::TILE_THREADS))
-        return launch_gated_generic<OP>(g, st);
-    Tiles tiles = quickest_tiles(g.Mo, (int)cols, (int)red);
-    if (tiles == Tiles::tall) tiles = tiles_in(g.Mo, 64) * tiles_in((int)cols, 128) <= NUM_CU ? Tiles::wide : Tiles::mid;
-    return gated_plain<OP>(g) ? launch_gated_on<OP, true>(g, tiles, (int)cols, (int)red, st) : launch_gated_on<OP, false>(g, tiles, (int)cols, (int)red, st);
+GatedCut gated_cut(int Mo, int No, int R, double* us) {
+    const int64_t chunks = steps_in(R) * (OP == axo::GATED_DX ? 2 : 1);
+    const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);  // MB
+    GatedCut best;
+    *us = 1e30;
+    for (int k = 0; k < 3; ++k) {
+        const GatedSlim& m = GATED_SLIM[OP][k];
+        if (m.rows == 0 || (m.rows == 16 && Mo > 256)) continue;
+        const int64_t tm = tiles_in(Mo, m.rows), tn = tiles_in(No, m.cols), tiles = tm * tn;
+        if (tiles > 4000) continue;
+        const int cols = m.cols * (OP == axo::GATED_FWD ? 2 : 1);
+        const double stage = (m.rows + cols) * 128 / 1024.0;
+        const int64_t lds = std::max<int64_t>(m.stages * (m.rows + cols) * 128, m.rows * (cols + 4) * 4) * m.waves;
+        const int64_t beside = std::min<int64_t>(8, 160 * 1024 / lds);  // workgroups on a CU
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (s > 1 && (tiles * s > GATED_MOST_WORKGROUPS || chunks < 4 * s)) break;
+            const int64_t per = (chunks + s - 1) / s, slices = (chunks + per - 1) / per, rounds = rounds_of(tiles * slices);
+            const double share = rounds * (per * stage / m.rate + m.each);
+            const double chain = (double)((per + m.waves - 1) / m.waves) * m.latency / m.stages * ((rounds + beside - 1) / beside);
+            const double t = m.fixed + std::max({share, chain, weights / m.tbs}) + (slices > 1 ? m.join + slices * m.per_slice : 0.0);
+            if (t >= *us) continue;
+            *us = t;
+            best.kind = k;
+            best.tiles_m = tm;
+            best.tiles_n = tn;
+            best.slices = (int)slices;
+            best.chunks = (int)per;
+            best.bytes = slices > 1 ? GATED_COUNTER_BYTES + (size_t)(tiles * slices) * m.rows * cols * sizeof(float) : 0;
+        }
+    }
+    return best;
 }
 
-size_t gated_workspace(const Shard&) { return 0; }
+// What a product of a gated block runs on, from its sizes alone.
+struct GatedPlan {
+    bool general = false;
+    Tiles tiles = Tiles::big;
+    GatedCut cut;
+};
+template <int OP>
+GatedPlan gated_plan(int Mo, int No, int R) {
+    GatedPlan plan;
+    if (Mo == 0 || No == 0) return plan;
+    // as one product: twice the columns, or twice the reduction
+    const int64_t cols = OP == axo::GATED_FWD ? 2 * (int64_t)No : No, red = OP == axo::GATED_DX ? 2 * (int64_t)R : R;
+    if (R == 0 || cols > INT32_MAX || red > INT32_MAX || !grid_fits(tiles_in(Mo, 64) * tiles_in((int)cols, 64), axo::TILE_THREADS)) {
+        plan.general = true;
+        return plan;
+    }
+    plan.tiles = quickest_tiles(Mo, (int)cols, (int)red);
+    const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);
+    const double tiles_us = std::max(tiles_time(plan.tiles, Mo, (int)cols, (int)red) * GATED_TILES[OP][(int)plan.tiles], 3.0 + weights / 5.0);
+    if (plan.tiles == Tiles::tall) plan.tiles = tiles_in(Mo, 64) * tiles_in((int)cols, 128) <= NUM_CU ? Tiles::wide : Tiles::mid;
+    if (Mo > 2048) return plan;  // never quicker there
+    double us;
+    const GatedCut cut = gated_cut<OP>(Mo, No, R, &us);
+    if (us < 0.9 * tiles_us) plan.cut = cut;
+    return plan;
+}
+
+template <int OP, int KIND>
+int launch_gated_slim(const GatedArgs& g, const GatedCut& cut, void* ws, hipStream_t st) {
+    constexpr GatedSlim M = GATED_SLIM[OP][KIND];
+    if constexpr (M.rows == 0) return AXO_ERR_BAD_ARG;
+    else {
+        using C = axo::GatedSlimCfg<OP, M.rows, M.cols, M.waves, M.stages>;
+        auto kern = axo::gated_slim_kernel<OP, M.rows, M.cols, M.waves, M.stages>;
+        static std::atomic<uint64_t> raised{0};
+        if (!raise_lds_limit(reinterpret_cast<const void*>(kern), C::LDS_BYTES, &raised)) return AXO_ERR_HIP;
+        axo::GatedSlimSched sc{};
+        sc.tiles_m = (int)cut.tiles_m;
+        sc.tiles_n = (int)cut.tiles_n;
+        sc.slices = cut.slices;
+        sc.chunks = cut.chunks;
+        sc.counters = static_cast<uint32_t*>(ws);
+        sc.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + GATED_COUNTER_BYTES);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(cut.tiles_m * cut.tiles_n * cut.slices)), dim3(C::THREADS), C::LDS_BYTES, st, axo::GatedProduct<OP>{g}, sc);
+        return launched();
+    }
+}
+template <int OP>
+int launch_gated(const GatedArgs& g, void* ws, hipStream_t st) {
+    if (g.Mo == 0 || g.No == 0) return AXO_OK;
+    const GatedPlan plan = gated_plan<OP>(g.Mo, g.No, g.R);
+    if (plan.general || !gated_spans_ok<OP>(g)) return launch_gated_generic<OP>(g, st);
+    switch (plan.cut.kind) {
+        case 0: return launch_gated_slim<OP, 0>(g, plan.cut, ws, st);
+        case 1: return launch_gated_slim<OP, 1>(g, plan.cut, ws, st);
+        case 2: return launch_gated_slim<OP, 2>(g, plan.cut, ws, st);
+        default: break;
+    }
+    const int cols = OP == axo::GATED_FWD ? 2 * g.No : g.No, red = OP == axo::GATED_DX ? 2 * g.R : g.R;
+    return gated_plain<OP>(g) ? launch_gated_on<OP, true>(g, plan.tiles, cols, red, st) : launch_gated_on<OP, false>(g, plan.tiles, cols, red, st);
+}
+
+// The largest workspace of the calls that a problem is passed to: as the block's projections and as the layer behind it.
+size_t gated_workspace(const Shard& s) {
+    if (s.M == 0 || s.Kl == 0 || s.Nl == 0) return 0;
+    const int M = (int)s.M, K = (int)s.Kl, N = (int)s.Nl;
+    return std::max({gated_plan<axo::GATED_FWD>(M, N, K).cut.bytes, gated_plan<axo::GATED_DX>(M, K, N).cut.bytes, gated_plan<axo::GATED_DACT>(M, K, N).cut.bytes});
+}
 int check_gated_workspace(const Shard& s, const void* ws, size_t ws_bytes, Buffers& b) {
     const size_t need = gated_workspace(s);
     if (need == 0) return AXO_OK;
@@ -466,7 +589,7 @@ int axo_gated_fwd(const axo_problem_t* p, const void* X, int64_t ldx, const void
         g.ldz = ldz;
         g.Mo = (int)s.M; g.No = (int)s.Nl; g.R = (int)s.Kl;
         g.gate = gate;
-        return launch_gated<axo::GATED_FWD>(g, static_cast<hipStream_t>(hip_stream));
+        return launch_gated<axo::GATED_FWD>(g, ws, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -548,7 +671,7 @@ int axo_gated_dgrad_act(const axo_problem_t* p, const void* dY, int64_t lddy, co
         g.aux2 = static_cast<const bf16_t*>(U);
         g.Mo = (int)s.M; g.No = (int)s.Kl; g.R = (int)s.Nl;
         g.gate = gate;
-        return launch_gated<axo::GATED_DACT>(g, static_cast<hipStream_t>(hip_stream));
+        return launch_gated<axo::GATED_DACT>(g, ws, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -575,7 +698,7 @@ int axo_gated_dgrad(const axo_problem_t* p, const void* dG, const void* dU, int6
         g.B2 = static_cast<const bf16_t*>(Wu);
         g.C = static_cast<bf16_t*>(dX); g.ldc = lddx;
         g.Mo = (int)s.M; g.No = (int)s.Kl; g.R = (int)s.Nl;
-        return launch_gated<axo::GATED_DX>(g, static_cast<hipStream_t>(hip_stream));
+        return launch_gated<axo::GATED_DX>(g, ws, static_cast<hipStream_t>(hip_stream));
     });
 }
 

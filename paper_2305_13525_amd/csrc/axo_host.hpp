@@ -137,6 +137,7 @@ int launch_products(const axo::GemmArgs* products, int n, int la, int lb, hipStr
 // half-width ones, start-up shift included (defined beside the planners).
 enum class Tiles { small, wide, tall, mid, big };
 Tiles quickest_tiles(int Mo, int No, int R);
+double tiles_time(Tiles tiles, int Mo, int No, int R);  // estimate in us, operands in the caches
 axo::TileSched plan_columns(int Mo, int No, int R);
 
 }  // namespace axo_host

@@ -46,7 +46,7 @@ struct SlimOperand {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int q = j * 64 + lane;
-            if (LAYOUT == KC) {
+            if constexpr (LAYOUT == KC) {
                 const int r = q >> 3, cs = q & 7;
                 off[j] = (uint32_t)(((int64_t)r * ld + ((cs ^ swz_kc(r)) << 3)) * 2);
             } else {
@@ -55,7 +55,7 @@ struct SlimOperand {
                 off[j] = (uint32_t)(((int64_t)k * ld + ((cs ^ swz_mc<ROWS>(k)) << 3)) * 2);
             }
         }
-        if (LAYOUT == KC) {
+        if constexpr (LAYOUT == KC) {
             const int r = lane & 15;
 #pragma unroll
             for (int kq = 0; kq < 2; ++kq) addr[kq] = r * (TILE_BK * 2) + (((kq * 4 + (lane >> 4)) ^ swz_kc(r)) << 4);
@@ -70,7 +70,7 @@ struct SlimOperand {
     }
     // fragment of MFMA tile t, 32-wide sub-step kq, of the stage at `stage`
     __device__ __forceinline__ bf16x8 read(const char* stage, int t, int kq) const {
-        if (LAYOUT == KC) {
+        if constexpr (LAYOUT == KC) {
             return *reinterpret_cast<const bf16x8*>(stage + addr[kq] + t * (16 * TILE_BK * 2));
         } else {
             typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
