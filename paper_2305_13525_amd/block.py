@@ -1,11 +1,12 @@
-"""ctypes binding of layer norm and the gated feed-forward block (include/axo_block.h): argument marshalling only, same names and argument
-order as the C functions, matrices as raw device addresses, streams as raw `hipStream_t` values."""
+"""Binding of layer norm and the gated feed-forward block (include/axo_block.h): argument marshalling only, same names and argument order as
+the C functions, matrices as raw device addresses, streams as raw `hipStream_t` values.  By ctypes, and through the extension module _calls,
+whose functions stand in for the wrappers below and call them for all but plain arguments."""
 from __future__ import annotations
 
 import ctypes
 from typing import Optional
 
-from .binding import Problem, _check, library
+from .binding import Problem, _calls, _check, library
 
 AXO_TYPE_BF16, AXO_TYPE_F32 = 0, 1
 AXO_GATE_SILU, AXO_GATE_GELU_TANH, AXO_GATE_GELU_ERF = 0, 1, 2
@@ -28,6 +29,7 @@ _SIGNATURES = {
 }
 _KINDS = {"p": ctypes.POINTER(Problem), "v": ctypes.c_void_p, "l": ctypes.c_int64, "i": ctypes.c_int, "f": ctypes.c_float, "z": ctypes.c_size_t}
 
+_quick = _calls if hasattr(_calls, "bind_block") else None  # a module of an older build, or none, has not these functions
 _ready = None
 
 
@@ -41,6 +43,8 @@ def _lib():
         for name in ("axo_norm_workspace_bytes", "axo_gated_workspace_bytes"):
             getattr(L, name).argtypes = [_KINDS["p"]]
             getattr(L, name).restype = ctypes.c_size_t
+        if _quick is not None:
+            _quick.bind_block({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _SIGNATURES}, L.axo_version())
         _ready = L
     return _ready
 
@@ -135,3 +139,9 @@ def axo_gated_wgrad_acc(p: Problem, X: int, ldx: int, dG: int, dU: int, lddz: in
                         ws_bytes: int = 0, stream: Optional[int] = None, check: bool = True) -> int:
     rc = _lib().axo_gated_wgrad_acc(_ref(p), X, ldx, dG, dU, lddz, dWg, dWu, lddw, ws, ws_bytes, stream)
     return _check(rc, "axo_gated_wgrad_acc", check)
+
+
+_WRAPPERS = {name: globals()[name] for name in _SIGNATURES}
+if _quick is not None:
+    _quick.set_up_block(Problem, _WRAPPERS, _check)
+    globals().update({name: getattr(_quick, name) for name in _SIGNATURES})

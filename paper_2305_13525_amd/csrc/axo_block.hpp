@@ -366,6 +366,28 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     return plan;
 }
 
+// The plans of the calls that a problem is passed to, as the block's projections and as the layer behind it, and the largest workspace among them.  A
+// plan takes a microsecond; a thread keeps those of the problems that it called last.
+struct GatedPlans {
+    int64_t M = -1, K = -1, N = -1;
+    GatedPlan of[3];
+    size_t bytes = 0;
+};
+const GatedPlans& gated_plans(const Shard& s) {
+    static thread_local GatedPlans kept[16];
+    GatedPlans& p = kept[(size_t)(s.M + 31 * s.Kl + 1009 * s.Nl) % 16];
+    if (p.M == s.M && p.K == s.Kl && p.N == s.Nl) return p;
+    const int M = (int)s.M, K = (int)s.Kl, N = (int)s.Nl;
+    p.of[axo::GATED_FWD] = gated_plan<axo::GATED_FWD>(M, N, K);
+    p.of[axo::GATED_DACT] = gated_plan<axo::GATED_DACT>(M, K, N);
+    p.of[axo::GATED_DX] = gated_plan<axo::GATED_DX>(M, K, N);
+    p.bytes = std::max({p.of[0].cut.bytes, p.of[1].cut.bytes, p.of[2].cut.bytes});
+    p.M = s.M;
+    p.K = s.Kl;
+    p.N = s.Nl;
+    return p;
+}
+
 template <int OP, int KIND>
 int launch_gated_slim(const GatedArgs& g, const GatedCut& cut, void* ws, hipStream_t st) {
     constexpr GatedSlim M = GATED_SLIM[OP][KIND];
@@ -387,9 +409,9 @@ int launch_gated_slim(const GatedArgs& g, const GatedCut& cut, void* ws, hipStre
     }
 }
 template <int OP>
-int launch_gated(const GatedArgs& g, void* ws, hipStream_t st) {
+int launch_gated(const GatedArgs& g, const Shard& s, void* ws, hipStream_t st) {
     if (g.Mo == 0 || g.No == 0) return AXO_OK;
-    const GatedPlan plan = gated_plan<OP>(g.Mo, g.No, g.R);
+    const GatedPlan& plan = gated_plans(s).of[OP];
     if (plan.general || !gated_spans_ok<OP>(g)) return launch_gated_generic<OP>(g, st);
     switch (plan.cut.kind) {
         case 0: return launch_gated_slim<OP, 0>(g, plan.cut, ws, st);
@@ -401,14 +423,8 @@ int launch_gated(const GatedArgs& g, void* ws, hipStream_t st) {
     return gated_plain<OP>(g) ? launch_gated_on<OP, true>(g, plan.tiles, cols, red, st) : launch_gated_on<OP, false>(g, plan.tiles, cols, red, st);
 }
 
-// The largest workspace of the calls that a problem is passed to: as the block's projections and as the layer behind it.
-size_t gated_workspace(const Shard& s) {
-    if (s.M == 0 || s.Kl == 0 || s.Nl == 0) return 0;
-    const int M = (int)s.M, K = (int)s.Kl, N = (int)s.Nl;
-    return std::max({gated_plan<axo::GATED_FWD>(M, N, K).cut.bytes, gated_plan<axo::GATED_DX>(M, K, N).cut.bytes, gated_plan<axo::GATED_DACT>(M, K, N).cut.bytes});
-}
 int check_gated_workspace(const Shard& s, const void* ws, size_t ws_bytes, Buffers& b) {
-    const size_t need = gated_workspace(s);
+    const size_t need = gated_plans(s).bytes;
     if (need == 0) return AXO_OK;
     if (!ws || ws_bytes < need) return AXO_ERR_WORKSPACE;
     if (!aligned16(ws)) return AXO_ERR_MISALIGNED;
@@ -589,7 +605,7 @@ int axo_gated_fwd(const axo_problem_t* p, const void* X, int64_t ldx, const void
         g.ldz = ldz;
         g.Mo = (int)s.M; g.No = (int)s.Nl; g.R = (int)s.Kl;
         g.gate = gate;
-        return launch_gated<axo::GATED_FWD>(g, ws, static_cast<hipStream_t>(hip_stream));
+        return launch_gated<axo::GATED_FWD>(g, s, ws, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -671,7 +687,7 @@ int axo_gated_dgrad_act(const axo_problem_t* p, const void* dY, int64_t lddy, co
         g.aux2 = static_cast<const bf16_t*>(U);
         g.Mo = (int)s.M; g.No = (int)s.Kl; g.R = (int)s.Nl;
         g.gate = gate;
-        return launch_gated<axo::GATED_DACT>(g, ws, static_cast<hipStream_t>(hip_stream));
+        return launch_gated<axo::GATED_DACT>(g, s, ws, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -698,7 +714,7 @@ int axo_gated_dgrad(const axo_problem_t* p, const void* dG, const void* dU, int6
         g.B2 = static_cast<const bf16_t*>(Wu);
         g.C = static_cast<bf16_t*>(dX); g.ldc = lddx;
         g.Mo = (int)s.M; g.No = (int)s.Kl; g.R = (int)s.Nl;
-        return launch_gated<axo::GATED_DX>(g, ws, static_cast<hipStream_t>(hip_stream));
+        return launch_gated<axo::GATED_DX>(g, s, ws, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -718,7 +734,7 @@ int axo_gated_wgrad_acc(const axo_problem_t* p, const void* X, int64_t ldx, cons
 
 size_t axo_gated_workspace_bytes(const axo_problem_t* p) {
     axo_host::Shard s;
-    return axo_host::derive_shard(p, &s) ? 0 : axo_block::gated_workspace(s);
+    return axo_host::derive_shard(p, &s) ? 0 : axo_block::gated_plans(s).bytes;
 }
 
 }  // extern "C"

@@ -247,3 +247,41 @@ def test_activations():
     assert abs(ob.gate(np.array([1.0]), 0)[0][0] - 1.0 / (1.0 + math.exp(-1.0))) < 1e-15
     assert abs(ob.gate(np.array([1.0]), 2)[0][0] - 0.8413447460685429) < 1e-15
     assert abs(ob.gate(np.array([1.0]), 1)[0][0] - 0.8411919906082768) < 1e-12
+
+
+# ---- the extension module's calls against the ctypes wrappers ----
+
+def outcome(f, *a, **k):
+    try:
+        return f(*a, **k)
+    except Exception as e:  # noqa: BLE001
+        return type(e), str(e)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_quick_calls(name):
+    """The same status or exception for every form of arguments, none of which launches anything: two of them are wrong, or there are no elements."""
+    _calls = pytest.importorskip("paper_2305_13525_amd._calls", reason="the extension module is not built")
+    quick, wrapper = getattr(_calls, name), block._WRAPPERS[name]
+    assert getattr(axo, name) is quick and quick is not wrapper
+    axo.axo_gated_workspace_bytes(P())  # the library is loaded
+    plain = [None if isinstance(v, int) and v >= at(1) and k != "ws_bytes" else v for k, v in GOOD[name].items()]
+    empty = [P(T=0)] + plain[1:] if "wgrad" not in name else [P(T=0, K=0, N=0)] + plain[1:]
+    if "Wg" in GOOD[name] or "W" in GOOD[name]:
+        empty[0] = P(T=0, K=0, N=0)
+    assert outcome(quick, *empty) == outcome(wrapper, *empty) == 0
+    n = 0
+    for base in (empty, [P(grid=(0, 1, 1))] + plain[1:]):
+        for i in range(len(base)):
+            for v in (None, 1.5, "x", True, -1, 2 ** 31, 2 ** 63, 2 ** 64, 7):
+                args = list(base)
+                args[i] = v
+                if i == 0 and isinstance(v, int):
+                    continue
+                for tail in ((), (None, False) if len(base) == len(GOOD[name]) else ()):
+                    assert outcome(quick, *args, *tail, check=False) == outcome(wrapper, *args, *tail, check=False) if not tail else outcome(
+                        quick, *args, *tail) == outcome(wrapper, *args, *tail), (args, tail)
+                    n += 1
+        for m in range(len(base)):
+            assert outcome(quick, *base[:m]) == outcome(wrapper, *base[:m])
+    assert n > 100
