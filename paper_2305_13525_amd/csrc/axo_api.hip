@@ -1295,6 +1295,11 @@ axo::TileSched plan_columns(int Mo, int No, int R) {
     return sc;
 }
 
+int takes_lines_on(const GemmArgs& g, int la, int lb, Tiles tiles, const axo::TileSched& sc) {
+    if (tiles == Tiles::big) return lines_of(g, la, lb, sc);
+    return takes_lines(g, la, lb, tiles == Tiles::small ? Tile::t64 : Tile::t128) ? LINES_ALL : LINES_NONE;
+}
+
 }  // namespace axo_host
 
 extern "C" {

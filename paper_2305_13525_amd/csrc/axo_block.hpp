@@ -260,18 +260,41 @@ int launch_gated_tiles(Kernel kern, std::atomic<uint64_t>* raised, const GatedAr
     hipLaunchKernelGGL(kern, dim3((unsigned)tm * (unsigned)tn), dim3(C::THREADS), C::LDS_BYTES, st, args, tm, tn, std::min(tm, 8));
     return launched();
 }
-template <int OP, bool PLAIN>
-int launch_gated_on(const GatedArgs& g, Tiles tiles, int cols, int steps, hipStream_t st) {
+template <int OP, bool PLAIN, int LINES>
+int launch_gated_on(const GatedArgs& g, Tiles tiles, const axo::TileSched& sc, hipStream_t st) {
     static std::atomic<uint64_t> raised[4]{{0}, {0}, {0}, {0}};
-    if (tiles == Tiles::small) return launch_gated_tiles<axo::SmallCfg<false>, OP>(axo::gated_small_kernel<OP, PLAIN>, &raised[0], g, 64, 64, st);
-    if (tiles == Tiles::wide) return launch_gated_tiles<axo::RectCfg<true>, OP>(axo::gated_rect_kernel<OP, PLAIN>, &raised[1], g, 64, 128, st);
-    if (tiles == Tiles::mid) return launch_gated_tiles<axo::MidCfg, OP>(axo::gated_mid_kernel<OP, PLAIN>, &raised[2], g, 128, 128, st);
-    auto kern = axo::gated_mixed_kernel<OP, PLAIN>;
-    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), axo::MIX_LDS_BYTES, &raised[3])) return AXO_ERR_HIP;
-    const axo::TileSched sc = plan_columns(g.Mo, cols, steps);
-    hipLaunchKernelGGL(kern, dim3(sc.n_big + sc.tiles_m * sc.small_cols), dim3(axo::TILE_THREADS), axo::MIX_LDS_BYTES, st, axo::GatedProduct<OP>{g}, sc);
+    constexpr bool ALL = LINES == 2;
+    if constexpr (LINES != 1) {
+        if (tiles == Tiles::small) return launch_gated_tiles<axo::SmallCfg<ALL>, OP>(axo::gated_small_kernel<OP, PLAIN, ALL>, &raised[0], g, 64, 64, st);
+        if (tiles == Tiles::wide) return launch_gated_tiles<axo::RectCfg<true>, OP>(axo::gated_rect_kernel<OP, PLAIN, ALL>, &raised[1], g, 64, 128, st);
+        if (tiles == Tiles::mid) return launch_gated_tiles<axo::MidCfg, OP>(axo::gated_mid_kernel<OP, PLAIN, ALL>, &raised[2], g, 128, 128, st);
+    }
+    // Forward ring tiles fetch one operand by lines at most and half-width ones none (takes_lines), so there is no forward of kind 2 on 256-row tiles.
+    constexpr int MIXED = OP == axo::GATED_FWD && LINES == 2 ? 1 : LINES;
+    constexpr int lds = LINES != 0 ? axo::LINES_LDS_BYTES : axo::MIX_LDS_BYTES;
+    auto kern = axo::gated_mixed_kernel<OP, PLAIN, MIXED>;
+    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), lds, &raised[3])) return AXO_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3(sc.n_big + sc.tiles_m * sc.small_cols), dim3(axo::TILE_THREADS), lds, st, axo::GatedProduct<OP>{g}, sc);
     return launched();
 }
+// On the tiles of a plan.  Where rows of the inputs are fetched by whole lines those of the outputs mostly straddle lines as well, so there is one kind of
+// such kernels, with plain stores.  dX, whose two products may lie differently in their lines, does not do that, and its epilogue looks at the output itself.
+template <int OP>
+int launch_gated_tiles_of(const GatedArgs& g, Tiles tiles, int cols, int red, hipStream_t st) {
+    const axo::TileSched sc = tiles == Tiles::big ? plan_columns(g.Mo, cols, red) : axo::TileSched{};
+    if constexpr (OP == axo::GATED_DX) return launch_gated_on<OP, false, 0>(g, tiles, sc, st);
+    else {
+        axo::GemmArgs as_one = g;
+        as_one.No = cols;
+        switch (takes_lines_on(as_one, axo::KC, axo::GATED_LB<OP>, tiles, sc)) {
+            case 2: return launch_gated_on<OP, true, 2>(g, tiles, sc, st);
+            case 1: return launch_gated_on<OP, true, 1>(g, tiles, sc, st);
+            default: break;
+        }
+        return gated_plain<OP>(g) ? launch_gated_on<OP, true, 0>(g, tiles, sc, st) : launch_gated_on<OP, false, 0>(g, tiles, sc, st);
+    }
+}
+
 // ---- split reductions (gated_slim.hpp) ----
 // The workspace: arrival counters of at most so many tiles, and behind them the sums of the slices.
 constexpr size_t GATED_COUNTER_BYTES = 8192;
@@ -420,7 +443,7 @@ int launch_gated(const GatedArgs& g, const Shard& s, void* ws, hipStream_t st) {
         default: break;
     }
     const int cols = OP == axo::GATED_FWD ? 2 * g.No : g.No, red = OP == axo::GATED_DX ? 2 * g.R : g.R;
-    return gated_plain<OP>(g) ? launch_gated_on<OP, true>(g, plan.tiles, cols, red, st) : launch_gated_on<OP, false>(g, plan.tiles, cols, red, st);
+    return launch_gated_tiles_of<OP>(g, plan.tiles, cols, red, st);
 }
 
 int check_gated_workspace(const Shard& s, const void* ws, size_t ws_bytes, Buffers& b) {

@@ -137,7 +137,8 @@ constexpr int GATED_LB = OP == GATED_FWD ? MC : KC;
 template <int OP>
 constexpr int gated_cols(int BN) { return OP == GATED_FWD ? BN / 2 : BN; }  // of the output, in a tile of BN columns of B
 
-template <int OP, bool PLAIN>
+// LINES: rows by whole lines on no tiles (0), on the large ones (1), on both (2), as gemm_mixed_kernel.
+template <int OP, bool PLAIN, int LINES>
 __global__ void __launch_bounds__(TILE_THREADS, 1) gated_mixed_kernel(GatedProduct<OP> g, TileSched sc) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int LB = GATED_LB<OP>, BIG = gated_cols<OP>(256), HALF = gated_cols<OP>(128);
@@ -146,36 +147,36 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) gated_mixed_kernel(GatedProdu
     int tm, tn;
     if (bid < sc.n_big) {
         tile_of_index(xcd_run(bid, sc.n_big), sc.tiles_m, sc.big_cols, sc.group_m, tm, tn);
-        gemm_tile_body<256, 256, 2, 4, KC, LB, false, PLAIN>(g, inside_row<256, KC>(g, tm * 256), inside_col<BIG>(g, tn * BIG), smem);
+        gemm_tile_body<256, 256, 2, 4, KC, LB, LINES != 0, PLAIN>(g, inside_row<256, KC>(g, tm * 256), inside_col<BIG>(g, tn * BIG), smem);
     } else {
         const int n_small = (int)gridDim.x - sc.n_big;
         tile_of_index(xcd_run(bid - sc.n_big, n_small), sc.tiles_m, sc.small_cols, sc.group_m, tm, tn);
-        gemm_ring_body<256, 128, 4, 2, 3, KC, LB, false, PLAIN>(g, inside_row<256, KC>(g, tm * 256), inside_col<HALF>(g, sc.big_cols * BIG + tn * HALF), smem, threadIdx.x);
+        gemm_ring_body<256, 128, 4, 2, 3, KC, LB, LINES == 2, PLAIN>(g, inside_row<256, KC>(g, tm * 256), inside_col<HALF>(g, sc.big_cols * BIG + tn * HALF), smem, threadIdx.x);
     }
 }
-template <int OP, bool PLAIN>
+template <int OP, bool PLAIN, bool LINES>
 __global__ void __launch_bounds__(TILE_THREADS, 1) gated_mid_kernel(GatedProduct<OP> g, int tiles_m, int tiles_n, int group_m) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int COLS = gated_cols<OP>(128);
     int tm, tn;
     tile_of_index(xcd_run(blockIdx.x, gridDim.x), tiles_m, tiles_n, group_m, tm, tn);
-    gemm_ring_body<128, 128, 4, 2, 4, KC, GATED_LB<OP>, false, PLAIN>(g, inside_row<128, KC>(g, tm * 128), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
+    gemm_ring_body<128, 128, 4, 2, 4, KC, GATED_LB<OP>, LINES, PLAIN>(g, inside_row<128, KC>(g, tm * 128), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
 }
-template <int OP, bool PLAIN>
+template <int OP, bool PLAIN, bool LINES>
 __global__ void __launch_bounds__(TILE_THREADS, 1) gated_rect_kernel(GatedProduct<OP> g, int tiles_m, int tiles_n, int group_m) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int COLS = gated_cols<OP>(128);
     int tm, tn;
     tile_of_index(xcd_run(blockIdx.x, gridDim.x), tiles_m, tiles_n, group_m, tm, tn);
-    gemm_ring_body<64, 128, 2, 4, 4, KC, GATED_LB<OP>, false, PLAIN>(g, inside_row<64, KC>(g, tm * 64), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
+    gemm_ring_body<64, 128, 2, 4, 4, KC, GATED_LB<OP>, LINES, PLAIN>(g, inside_row<64, KC>(g, tm * 64), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
 }
-template <int OP, bool PLAIN>
+template <int OP, bool PLAIN, bool LINES>
 __global__ void __launch_bounds__(256, 2) gated_small_kernel(GatedProduct<OP> g, int tiles_m, int tiles_n, int group_m) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     constexpr int COLS = gated_cols<OP>(64);
     int tm, tn;
     tile_of_index(xcd_run(blockIdx.x, gridDim.x), tiles_m, tiles_n, group_m, tm, tn);
-    gemm_ring_body<64, 64, 2, 2, 4, KC, GATED_LB<OP>, false, PLAIN>(g, inside_row<64, KC>(g, tm * 64), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
+    gemm_ring_body<64, 64, 2, 2, LINES ? 5 : 4, KC, GATED_LB<OP>, LINES, PLAIN>(g, inside_row<64, KC>(g, tm * 64), inside_col<COLS>(g, tn * COLS), smem, threadIdx.x);
 }
 
 }  // namespace axo

@@ -991,52 +991,53 @@ __device__ __forceinline__ void gated_fwd_epilogue(const Args& g, f32x4 (&acc)[C
 }
 
 // Backward: dG = sum U act'(G), dU = sum act(G).  A wave stages its sums in fp32, 16 or 32 rows at a time, so that a lane then holds eight columns of a
-// row, reads G and U and stores both results 16 bytes at a time; what a pass reads is requested a pass ahead.
+// row, reads G and U and stores both results 16 bytes at a time; what a pass reads is requested two passes ahead.
 template <typename C, bool PLAIN, typename Args>
 __device__ __forceinline__ void gated_dact_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int wrow0, const int wcol0, const int wave, const int lane,
                                                     char* smem, const bool whole) {
     constexpr int F_STRIDE = C::WTN * 4 + 16, ROWS = C::TM * C::TN == 32 ? 16 : 32, LPR = C::WTN / 8, RPI = 64 / LPR, ITERS = ROWS / RPI, PASSES = C::WTM / ROWS;
-    static_assert(C::WAVES * ROWS * F_STRIDE <= C::LDS_BYTES && ROWS % RPI == 0, "fits the operand buffers");
+    static_assert(C::WAVES * ROWS * F_STRIDE <= C::LDS_BYTES && ROWS % RPI == 0 && PASSES <= 8, "fits the operand buffers");
     char* const stage = smem + wave * (ROWS * F_STRIDE);
     const int lr = lane / LPR, lc = lane % LPR * 8, col = wcol0 + lc, valid = g.No - col;
-    u32x4 gs[ITERS], us[ITERS];
-    auto request = [&](const int row0) __attribute__((always_inline)) {
+    constexpr int AHEAD = 2;  // passes
+    u32x4 gs[AHEAD + 1][ITERS], us[AHEAD + 1][ITERS];
+    auto request = [&](auto pass_tag) __attribute__((always_inline)) {
+        constexpr int pass = decltype(pass_tag)::value, s = pass % (AHEAD + 1);
+        const int row0 = wrow0 + pass * ROWS;
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {
             const int row = row0 + i * RPI + lr;
             const int64_t at = (int64_t)row * g.ldaux + col;
             if (whole || (row < g.Mo && valid >= 8)) {
-                gs[i] = *reinterpret_cast<const u32x4*>(g.aux + at);
-                us[i] = *reinterpret_cast<const u32x4*>(g.aux2 + at);
+                gs[s][i] = *reinterpret_cast<const u32x4*>(g.aux + at);
+                us[s][i] = *reinterpret_cast<const u32x4*>(g.aux2 + at);
             } else {
-                gs[i] = us[i] = u32x4{0u, 0u, 0u, 0u};
+                gs[s][i] = us[s][i] = u32x4{0u, 0u, 0u, 0u};
                 if (row < g.Mo)
 #pragma unroll
                     for (int e = 0; e < 7; ++e)
                         if (e < valid) {
-                            gs[i][e / 2] |= (uint32_t)g.aux[at + e] << (e % 2 * 16);
-                            us[i][e / 2] |= (uint32_t)g.aux2[at + e] << (e % 2 * 16);
+                            gs[s][i][e / 2] |= (uint32_t)g.aux[at + e] << (e % 2 * 16);
+                            us[s][i][e / 2] |= (uint32_t)g.aux2[at + e] << (e % 2 * 16);
                         }
             }
         }
     };
-    request(wrow0);
+    request(IC<0>{});
     __syncthreads();  // all waves are done reading the operand buffers
     with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            u32x4 gn[ITERS], un[ITERS];
-#pragma unroll
-            for (int i = 0; i < ITERS; ++i) {
-                gn[i] = gs[i];
-                un[i] = us[i];
-            }
-            if (p + 1 < PASSES) request(wrow0 + (p + 1) * ROWS);
+        auto pass = [&](auto p_tag) __attribute__((always_inline)) {
+            constexpr int p = decltype(p_tag)::value, s = p % (AHEAD + 1);
+            if constexpr (p >= PASSES) return;
+            else {
 #pragma unroll
             for (int a = 0; a < ROWS / 16; ++a)
 #pragma unroll
                 for (int b = 0; b < C::TN; ++b)
                     *reinterpret_cast<f32x4*>(stage + (a * 16 + (lane & 15)) * F_STRIDE + (b * 16 + 4 * (lane >> 4)) * 4) = acc[p * (ROWS / 16) + a][b];
+            // behind the staging, which frees the registers of the sums
+            if constexpr (p == 0 && PASSES > 1) request(IC<1>{});
+            if constexpr (p + AHEAD < PASSES) request(IC<p + AHEAD>{});
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the region is private to the wave
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -1047,8 +1048,8 @@ __device__ __forceinline__ void gated_dact_epilogue(const Args& g, f32x4 (&acc)[
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float s0 = e < 2 ? lo[2 * e] : hi[2 * e - 4], s1 = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
-                    const float2 a0 = gate_both<decltype(gate)::value>(__uint_as_float(gn[i][e] << 16)), a1 = gate_both<decltype(gate)::value>(__uint_as_float(gn[i][e] & 0xFFFF0000u));
-                    dg[e] = pack_bf16x2(s0 * __uint_as_float(un[i][e] << 16) * a0.y, s1 * __uint_as_float(un[i][e] & 0xFFFF0000u) * a1.y);
+                    const float2 a0 = gate_both<decltype(gate)::value>(__uint_as_float(gs[s][i][e] << 16)), a1 = gate_both<decltype(gate)::value>(__uint_as_float(gs[s][i][e] & 0xFFFF0000u));
+                    dg[e] = pack_bf16x2(s0 * __uint_as_float(us[s][i][e] << 16) * a0.y, s1 * __uint_as_float(us[s][i][e] & 0xFFFF0000u) * a1.y);
                     du[e] = pack_bf16x2(s0 * a0.x, s1 * a1.x);
                 }
                 if (whole || (row < g.Mo && valid > 0)) {
@@ -1058,7 +1059,16 @@ __device__ __forceinline__ void gated_dact_epilogue(const Args& g, f32x4 (&acc)[
                 }
             }
             __builtin_amdgcn_wave_barrier();  // LDS operations of a wave complete in order: the next pass may overwrite
-        }
+            }
+        };
+        pass(IC<0>{});
+        pass(IC<1>{});
+        pass(IC<2>{});
+        pass(IC<3>{});
+        pass(IC<4>{});
+        pass(IC<5>{});
+        pass(IC<6>{});
+        pass(IC<7>{});
     });
 }
 
