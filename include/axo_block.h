@@ -138,6 +138,15 @@ int axo_gated_wgrad_acc(const axo_problem_t *p, const void *X, int64_t ldx, cons
 /* Host only.  The largest workspace that any gated entry point needs when it is called with this problem; 0 for an invalid one. */
 size_t axo_gated_workspace_bytes(const axo_problem_t *p);
 
+/* The products of the block that have kernels of their own. */
+typedef enum axo_gated_op { AXO_GATED_OP_FWD = 0, AXO_GATED_OP_DGRAD_ACT = 1, AXO_GATED_OP_DGRAD = 2 } axo_gated_op_t;
+
+/* Host only.  How such a product is cut: rows and output columns of its tiles (of the largest, where there are two kinds), and the workgroups that share a
+ * tile's reduction (1: one).  Rows of 16 and 32 are those of tiles whose waves split the reduction; 0 rows, with 0 columns and 0 slices: an empty output, or the
+ * general kernel, which also takes operands whose spans pass 4 GiB, whatever is reported here.  A function of the shard's sizes alone, chosen by estimated time, so
+ * that the answer may change from one version to the next.  Errors: those of axo_shard_dims; BAD_ARG (op); NULL_PTR. */
+int axo_gated_tiles(const axo_problem_t *p, int op, int *rows, int *cols, int *slices);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,12 +4,13 @@ whose functions stand in for the wrappers below and call them for all but plain 
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+from typing import Optional, Tuple
 
 from .binding import Problem, _calls, _check, library
 
 AXO_TYPE_BF16, AXO_TYPE_F32 = 0, 1
 AXO_GATE_SILU, AXO_GATE_GELU_TANH, AXO_GATE_GELU_ERF = 0, 1, 2
+AXO_GATED_OP_FWD, AXO_GATED_OP_DGRAD_ACT, AXO_GATED_OP_DGRAD = 0, 1, 2
 
 # kinds of arguments: p problem, v pointer, l int64_t, i int, f float, z size_t
 _SIGNATURES = {
@@ -43,6 +44,8 @@ def _lib():
         for name in ("axo_norm_workspace_bytes", "axo_gated_workspace_bytes"):
             getattr(L, name).argtypes = [_KINDS["p"]]
             getattr(L, name).restype = ctypes.c_size_t
+        L.axo_gated_tiles.argtypes = [_KINDS["p"], ctypes.c_int] + 3 * [ctypes.POINTER(ctypes.c_int)]
+        L.axo_gated_tiles.restype = ctypes.c_int
         if _quick is not None:
             _quick.bind_block({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _SIGNATURES}, L.axo_version())
         _ready = L
@@ -59,6 +62,13 @@ def axo_norm_workspace_bytes(p: Problem) -> int:
 
 def axo_gated_workspace_bytes(p: Problem) -> int:
     return int(_lib().axo_gated_workspace_bytes(_ref(p)))
+
+
+def axo_gated_tiles(p: Problem, op: int, check: bool = True) -> Tuple[int, Tuple[int, int, int]]:
+    """(status, (rows, columns, workgroups per tile)) of the tiles that a product runs on."""
+    out = [ctypes.c_int(0) for _ in range(3)]
+    rc = _lib().axo_gated_tiles(_ref(p), op, *[ctypes.byref(o) for o in out])
+    return _check(rc, "axo_gated_tiles", check), tuple(o.value for o in out)
 
 
 def axo_norm_fwd(p: Problem, X: int, ldx: int, R: Optional[int], ldr: int, type: int, gamma: Optional[int], beta: Optional[int], eps: float,

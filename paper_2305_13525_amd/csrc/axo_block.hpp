@@ -10,6 +10,9 @@
 #include "gated_slim.hpp"
 #include "norm.hpp"
 
+static_assert((int)AXO_GATED_OP_FWD == axo::GATED_FWD && (int)AXO_GATED_OP_DGRAD_ACT == axo::GATED_DACT && (int)AXO_GATED_OP_DGRAD == axo::GATED_DX, "one numbering");
+static_assert((int)AXO_GATE_SILU == axo::GATE_SILU && (int)AXO_GATE_GELU_TANH == axo::GATE_GELU_TANH && (int)AXO_GATE_GELU_ERF == axo::GATE_GELU_ERF, "one numbering");
+
 namespace axo_block {
 
 using namespace axo_host;
@@ -298,26 +301,30 @@ int launch_gated_tiles_of(const GatedArgs& g, Tiles tiles, int cols, int red, hi
 // ---- split reductions (gated_slim.hpp) ----
 // The workspace: arrival counters of at most so many tiles, and behind them the sums of the slices.
 constexpr size_t GATED_COUNTER_BYTES = 8192;
-constexpr int64_t GATED_MOST_WORKGROUPS = 1400;  // of a launch whose tiles are sliced
+constexpr int64_t GATED_MOST_TILES = GATED_COUNTER_BYTES / sizeof(uint32_t);
 
 // A kind of split-reduction tile, and what a product on it takes in us: `fixed`, and the longest of
-//   - a CU's share of the workgroups, each of which takes in its operands at `rate` KB per us and costs `each` besides;
+//   - a CU's share of the workgroups, each of which costs `each` and takes in its operands at `rate` KB per us, or `alone` where it has the CU to itself;
 //   - one wave's chain of chunks, `latency` each, as many under way as it has stages;
 //   - the weights, read at `tbs` TB/s;
-// and where its reduction is sliced `join` and `per_slice` for each slice.  Fitted to 100 000 measured launches of 14 000 shapes (1 to 800 tokens, widths of 32 to
-// 16384, weights from memory) with 1 to 16 slices; half of the estimates are within 8 to 17 %, nine of ten within 45 %.
+// and `join` where its reduction is sliced.  Fitted to 14 000 shapes (1 to 800 tokens, widths of 32 to 16384, weights from memory) and for the kind that is left to
+// few rows and much weight to 1400 of those; half of the estimates are within 5 to 11 %, nine of ten within 28 %.
 struct GatedSlim {
     int rows, cols, waves, stages;  // `cols`: of the output
-    double fixed, rate, latency, tbs, join, per_slice, each;
+    double fixed, rate, alone, latency, tbs, join, each;
 };
-constexpr GatedSlim GATED_SLIM[3][3] = {
-    {{16, 32, 4, 3, 2.0, 53.9, 2.60, 3.25, 0.57, 0.43, 2.22}, {32, 32, 4, 3, 2.0, 51.3, 2.97, 2.66, 0.83, 0.70, 2.36}, {16, 128, 2, 2, 2.0, 67.1, 1.97, 4.70, 2.35, 0.97, 4.01}},
-    {{16, 32, 4, 3, 3.06, 94.1, 0.85, 5.59, 0.68, 0.20, 1.18}, {32, 32, 4, 3, 2.0, 84.0, 1.31, 4.26, 0.44, 0.36, 2.72}, {}},
-    {{16, 32, 4, 3, 2.75, 84.6, 0.31, 4.96, 0.81, 0.18, 0.84}, {32, 32, 4, 3, 2.0, 78.3, 1.37, 3.69, 0.38, 0.36, 2.19}, {}}};
+constexpr GatedSlim GATED_SLIM[3][4] = {
+    {{16, 32, 4, 3, 3.26, 39.4, 67.2, 2.37, 3.78, 2.31, 1.21}, {32, 32, 4, 3, 2.85, 42.6, 64.6, 2.99, 3.14, 3.92, 1.53},
+     {16, 64, 2, 4, 3.10, 51.8, 97.2, 2.65, 4.87, 3.79, 2.04}, {16, 128, 2, 2, 4.73, 49.3, 50.0, 3.14, 6.18, 4.74, 0.30}},
+    {{16, 32, 4, 3, 4.32, 87.9, 126.6, 0.88, 6.72, 1.20, 0.66}, {32, 32, 4, 3, 3.01, 73.9, 155.4, 1.44, 5.48, 2.59, 1.84}, {}, {}},
+    {{16, 32, 4, 3, 4.16, 71.8, 78.6, 1.04, 5.69, 0.71, 0.28}, {32, 32, 4, 3, 3.16, 87.1, 115.1, 1.50, 4.63, 2.34, 1.24}, {}, {}}};
+// Rows of 256 bytes of either weight (the fourth kind) are for tokens of one tile that read more than the caches hold: there they are the quickest, 1.2 times quicker than 64 x 128
+// tiles (1 x 8192 x 16384 97 us, with rows of 128 bytes 109, on those tiles 104; where rows lie a multiple of 4 KiB apart, a column of 128 bytes
+// lies in half of each of its DRAM pages).  With less to read they are not.
+constexpr double GATED_WIDE_MB = 200.0;
 // The same for the tiles of gemm_tile.hpp: what their estimates have to be multiplied with for these products (small, wide, tall, mid, big; medians of the same
-// shapes), which read weights from memory and have longer epilogues.  They are taken unless a split reduction is estimated at least a tenth quicker:
-// over those shapes the choice is 1.35 (forward), 1.56 and 1.91 times quicker than these tiles throughout, 4 to 7 % slower than the best of all, and by more than 5 % slower
-// than these tiles for one or two shapes in a hundred.
+// shapes), which read weights from memory and have longer epilogues.  Whatever is estimated quicker is taken: over those shapes the choice is 1.29 (forward), 1.63 and 1.99 times
+// quicker than these tiles throughout, 3 to 5 % slower than the best of all, and by more than 5 % slower than these tiles for two or three shapes in a hundred.
 constexpr double GATED_TILES[3][5] = {{1.06, 1.66, 1.66, 1.21, 1.03}, {0.93, 1.37, 1.37, 1.41, 1.55}, {0.88, 1.47, 1.47, 1.21, 1.08}};
 
 // How a product is cut into split-reduction tiles.
@@ -327,6 +334,10 @@ struct GatedCut {
     int slices = 1, chunks = 0;
     size_t bytes = 0;  // of workspace
 };
+// Slices of a reduction: as many as leave every workgroup a CU to itself and sixteen chunks, within 1 to 4 % of the best number over those shapes (two workgroups per CU: 3 to 9 %
+// off, eight chunks 3 to 7 %).
+int64_t gated_slices(int64_t tiles, int64_t chunks) { return std::max<int64_t>(1, std::min<int64_t>({NUM_CU / tiles, chunks / 16, 16})); }
+
 // The quickest cut of a product (Mo x No, reductions of R) and the estimate of it.
 template <int OP>
 GatedCut gated_cut(int Mo, int No, int R, double* us) {
@@ -334,33 +345,32 @@ GatedCut gated_cut(int Mo, int No, int R, double* us) {
     const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);  // MB
     GatedCut best;
     *us = 1e30;
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
         const GatedSlim& m = GATED_SLIM[OP][k];
-        if (m.rows == 0 || (m.rows == 16 && Mo > 256)) continue;
+        if (m.rows == 0 || (m.rows == 16 && Mo > 256) || (k == 3 && (Mo > 16 || weights < GATED_WIDE_MB))) continue;
         const int64_t tm = tiles_in(Mo, m.rows), tn = tiles_in(No, m.cols), tiles = tm * tn;
         if (tiles > 4000) continue;
         const int cols = m.cols * (OP == axo::GATED_FWD ? 2 : 1);
         const double stage = (m.rows + cols) * 128 / 1024.0;
         const int64_t lds = std::max<int64_t>(m.stages * (m.rows + cols) * 128, m.rows * (cols + 4) * 4) * m.waves;
         const int64_t beside = std::min<int64_t>(8, 160 * 1024 / lds);  // workgroups on a CU
-        for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if (s > 1 && (tiles * s > GATED_MOST_WORKGROUPS || chunks < 4 * s)) break;
-            const int64_t per = (chunks + s - 1) / s, slices = (chunks + per - 1) / per, rounds = rounds_of(tiles * slices);
-            const double share = rounds * (per * stage / m.rate + m.each);
-            const double chain = (double)((per + m.waves - 1) / m.waves) * m.latency / m.stages * ((rounds + beside - 1) / beside);
-            const double t = m.fixed + std::max({share, chain, weights / m.tbs}) + (slices > 1 ? m.join + slices * m.per_slice : 0.0);
-            if (t >= *us) continue;
-            *us = t;
-            best.kind = k;
-            best.tiles_m = tm;
-            best.tiles_n = tn;
-            best.slices = (int)slices;
-            best.chunks = (int)per;
-            best.bytes = slices > 1 ? GATED_COUNTER_BYTES + (size_t)(tiles * slices) * m.rows * cols * sizeof(float) : 0;
-        }
+        const int64_t asked = gated_slices(tiles, chunks), per = (chunks + asked - 1) / asked, slices = (chunks + per - 1) / per;
+        const int64_t rounds = rounds_of(tiles * slices);
+        const double share = rounds * (per * stage / (rounds > 1 ? m.rate : m.alone) + m.each);
+        const double chain = (double)((per + m.waves - 1) / m.waves) * m.latency / m.stages * ((rounds + beside - 1) / beside);
+        const double t = m.fixed + std::max({share, chain, weights / m.tbs}) + (slices > 1 ? m.join : 0.0);
+        if (t >= *us) continue;
+        *us = t;
+        best.kind = k;
+        best.tiles_m = tm;
+        best.tiles_n = tn;
+        best.slices = (int)slices;
+        best.chunks = (int)per;
+        best.bytes = slices > 1 ? GATED_COUNTER_BYTES + (size_t)(tiles * slices) * m.rows * cols * sizeof(float) : 0;
     }
     return best;
 }
+static_assert(NUM_CU <= GATED_MOST_TILES, "a counter for every tile that is sliced");
 
 // What a product of a gated block runs on, from its sizes alone.
 struct GatedPlan {
@@ -385,7 +395,7 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     if (Mo > 2048) return plan;  // never quicker there
     double us;
     const GatedCut cut = gated_cut<OP>(Mo, No, R, &us);
-    if (us < 0.9 * tiles_us) plan.cut = cut;
+    if (us < tiles_us) plan.cut = cut;
     return plan;
 }
 
@@ -440,6 +450,7 @@ int launch_gated(const GatedArgs& g, const Shard& s, void* ws, hipStream_t st) {
         case 0: return launch_gated_slim<OP, 0>(g, plan.cut, ws, st);
         case 1: return launch_gated_slim<OP, 1>(g, plan.cut, ws, st);
         case 2: return launch_gated_slim<OP, 2>(g, plan.cut, ws, st);
+        case 3: return launch_gated_slim<OP, 3>(g, plan.cut, ws, st);
         default: break;
     }
     const int cols = OP == axo::GATED_FWD ? 2 * g.No : g.No, red = OP == axo::GATED_DX ? 2 * g.R : g.R;
@@ -758,6 +769,30 @@ int axo_gated_wgrad_acc(const axo_problem_t* p, const void* X, int64_t ldx, cons
 size_t axo_gated_workspace_bytes(const axo_problem_t* p) {
     axo_host::Shard s;
     return axo_host::derive_shard(p, &s) ? 0 : axo_block::gated_plans(s).bytes;
+}
+
+int axo_gated_tiles(const axo_problem_t* p, int op, int* rows, int* cols, int* slices) {
+    using namespace axo_block;
+    return guarded([&]() -> int {
+        Shard s;
+        if (const int rc = derive_shard(p, &s)) return rc;
+        if (op < AXO_GATED_OP_FWD || op > AXO_GATED_OP_DGRAD) return AXO_ERR_BAD_ARG;
+        if (!rows || !cols || !slices) return AXO_ERR_NULL_PTR;
+        *rows = *cols = *slices = 0;
+        if (s.M == 0 || (op == AXO_GATED_OP_FWD ? s.Nl : s.Kl) == 0) return AXO_OK;
+        const GatedPlan& plan = gated_plans(s).of[op];
+        if (plan.general) return AXO_OK;
+        *slices = plan.cut.slices;
+        if (plan.cut.kind >= 0) {
+            *rows = GATED_SLIM[op][plan.cut.kind].rows;
+            *cols = GATED_SLIM[op][plan.cut.kind].cols;
+            return AXO_OK;
+        }
+        const int wide = plan.tiles == Tiles::small ? 64 : plan.tiles == Tiles::big ? 256 : 128;
+        *rows = plan.tiles == Tiles::wide ? 64 : wide;
+        *cols = op == AXO_GATED_OP_FWD ? wide / 2 : wide;
+        return AXO_OK;
+    });
 }
 
 }  // extern "C"

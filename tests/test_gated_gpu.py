@@ -72,6 +72,39 @@ def test_forward_whole_tiles(m, k, f, kind):
     check_forward(inputs(m, k, f, kind), kind, kind != 1, (kind != 2, kind != 2))
 
 
+# (op, rows, columns, whether workgroups share a tile) -> tokens x width x inner width that run on such tiles, whole chunks and odd ones
+VARIANTS = [
+    (0, 16, 32, False, (1, 704, 8)), (0, 16, 32, False, (1, 663, 9)), (0, 16, 32, True, (1, 2048, 8)), (0, 16, 32, True, (2, 2016, 9)),
+    (0, 16, 64, False, (1, 64, 8232)), (0, 16, 64, False, (1, 8, 8486)), (0, 16, 64, True, (2, 5120, 1336)), (0, 16, 64, True, (1, 4095, 1566)),
+    (0, 16, 128, False, (1, 3328, 16608)), (0, 16, 128, True, (1, 4618, 10914)),
+    (0, 32, 32, False, (290, 1280, 8)), (0, 32, 32, False, (268, 975, 10)), (0, 32, 32, True, (321, 2304, 8)), (0, 32, 32, True, (270, 2004, 10)),
+    (0, 64, 32, False, (1, 64, 8)), (0, 64, 32, False, (1, 8, 9)), (0, 64, 64, False, (3, 1024, 14565)), (0, 64, 64, False, (1, 964, 14028)),
+    (0, 128, 64, False, (17, 64, 8880)), (0, 128, 64, False, (20, 8, 8199)), (0, 256, 128, False, (133, 64, 9416)), (0, 256, 128, False, (137, 8, 9259)),
+    (1, 16, 32, False, (2, 1920, 8)), (1, 16, 32, False, (1, 1840, 9)), (1, 16, 32, True, (1, 2048, 8)), (1, 16, 32, True, (2, 2016, 9)),
+    (1, 32, 32, False, (1, 768, 8)), (1, 32, 32, False, (1, 705, 9)), (1, 32, 32, True, (351, 2112, 8)), (1, 32, 32, True, (258, 2073, 9)),
+    (1, 64, 64, False, (1, 64, 8)), (1, 64, 64, False, (1, 8, 9)), (1, 64, 128, False, (23, 1088, 19000)), (1, 64, 128, False, (20, 961, 18788)),
+    (1, 128, 128, False, (21, 64, 17144)), (1, 128, 128, False, (19, 8, 16533)), (1, 256, 256, False, (144, 64, 16512)), (1, 256, 256, False, (129, 8, 17245)),
+    (2, 16, 32, False, (2, 64, 840)), (2, 16, 32, False, (1, 9, 806)), (2, 16, 32, True, (1, 64, 968)), (2, 16, 32, True, (1, 9, 961)),
+    (2, 32, 32, False, (1, 64, 360)), (2, 32, 32, False, (2, 9, 354)), (2, 32, 32, True, (294, 64, 992)), (2, 32, 32, True, (272, 10, 962)),
+    (2, 64, 64, False, (1, 64, 8)), (2, 64, 64, False, (1, 9, 8)), (2, 64, 128, False, (3904, 320, 504)), (2, 64, 128, False, (3678, 282, 481)),
+    (2, 128, 128, False, (85, 8640, 8)), (2, 128, 128, False, (82, 8423, 8)), (2, 256, 256, False, (404, 8384, 8)), (2, 256, 256, False, (397, 8315, 8))]
+
+
+@pytest.mark.parametrize("op,rows,cols,shared,size", VARIANTS)
+def test_every_kind_of_tiles(op, rows, cols, shared, size):
+    m, k, f = size
+    p = bu.problem(m, f, k) if op == axo.AXO_GATED_OP_DGRAD_ACT else bu.problem(m, k, f)
+    got = axo.axo_gated_tiles(p, op)[1]
+    assert got[:2] == (rows, cols) and (got[2] > 1) == shared, got
+    kind, gap = (m + f) % 3, (0, 8)[(k + f) % 2]
+    if op == axo.AXO_GATED_OP_FWD:
+        check_forward(inputs(m, k, f, 31), kind, save=f < 10000, gap=gap)
+    elif op == axo.AXO_GATED_OP_DGRAD_ACT:
+        check_dgrad_act(back_inputs(m, f, k, 32), kind, gap)
+    else:
+        check_products(m, k, f, 33, gap)
+
+
 def test_forward_no_reduction():
     """Kl = 0: act(bg) * bu."""
     d = inputs(5, 0, 40, 1)
