@@ -398,3 +398,32 @@ def test_same_bits_on_any_stream_and_in_graphs(m, k, f):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, t.view()) for a, t in zip(eager, outs)), turn
+
+
+def test_calls_share_a_workspace():
+    """Calls of several shapes, cut into different numbers of slices, one behind the other on one workspace: each gets what it gets on its own."""
+    shapes = [(1, 4096, 192), (2, 5120, 1336), (1, 9, 961), (40, 2104, 64), (1, 4095, 1566), (1, 2048, 8), (272, 10, 962)]
+    shared = [axo.axo_gated_tiles(bu.problem(m, k, f), op)[1][2] > 1 for m, k, f in shapes for op in (0, 2)]
+    assert sum(shared) >= 6
+    cases, need = [], 0
+    for m, k, f in shapes:
+        d, p = inputs(m, k, f, m + k), bu.problem(m, k, f)
+        rng = np.random.default_rng(k)
+        dz = bu.draw(rng, m, f), bu.draw(rng, m, f)
+        t = [bu.Mat(a) for a in (d["x"], d["wg"], d["wu"], *dz)]
+        need = max(need, axo.axo_gated_workspace_bytes(p))
+        cases.append((p, t, (m, k, f)))
+
+    def run(p, t, size, ws, n):
+        X, Wg, Wu, dG, dU = t
+        H, dX = bu.Out(size[0], size[2]), bu.Out(size[0], size[1])
+        axo.axo_gated_fwd(p, X.ptr, X.ld, Wg.ptr, Wu.ptr, Wg.ld, None, None, 0, None, None, 0, H.ptr, H.ld, ws.data_ptr(), n, bu.stream())
+        axo.axo_gated_dgrad(p, dG.ptr, dU.ptr, dG.ld, Wg.ptr, Wu.ptr, Wg.ld, dX.ptr, dX.ld, ws.data_ptr(), n, bu.stream())
+        return H, dX
+
+    alone = [run(*c, *workspace(c[0])) for c in cases]
+    ws = torch.zeros(need, dtype=torch.uint8, device=bu.DEV)
+    for turn in range(3):
+        for c, want in zip(cases[::-1] if turn % 2 else cases, alone[::-1] if turn % 2 else alone):
+            got = run(*c, ws, need)
+            assert all(np.array_equal(a.result(), b.result()) for a, b in zip(got, want)), (turn, c[2])
