@@ -55,7 +55,7 @@ typedef enum axo_gate {
  * gamma, beta: K bf16 values, or NULL for ones and zeros.  Y: bf16.  stats: M pairs of fp32 (mean, rstd) for the backward
  * pass, 8-byte aligned, or NULL.  eps >= 0 and finite.  K == 0: nothing is written.
  * Errors: those of axo_shard_dims; BAD_GRID (also for a K axis larger than 1); BAD_ARG (type, eps, shared bytes); NULL_PTR, BAD_LD, MISALIGNED; HIP.
- * Speed: one pass over the data for rows of up to 32768 values. */
+ * Speed: one pass over the data for rows of up to 32768 bf16 or 24576 fp32 values. */
 int axo_norm_fwd(const axo_problem_t *p, const void *X, int64_t ldx, const void *R, int64_t ldr, int type, const void *gamma,
                  const void *beta, float eps, void *S, int64_t lds, void *Y, int64_t ldy, float *stats, void *hip_stream);
 

@@ -63,7 +63,7 @@ int elem_of(int type) { return type == AXO_TYPE_F32 ? 4 : 2; }
 bool known_type(int type) { return type == AXO_TYPE_BF16 || type == AXO_TYPE_F32; }
 bool valid_eps(float eps) { return eps >= 0.0f && std::isfinite(eps); }
 
-// A workgroup to a row; more rows than this are walked.
+// A workgroup to a row or a piece of columns; more of them than this are walked (a grid has fewer than 2^32 threads).
 constexpr int64_t NORM_MOST_BLOCKS = 1 << 20;
 
 template <typename T, int LANES, int CH>
@@ -72,6 +72,13 @@ int launch_norm_rows(const axo::NormArgs& g, hipStream_t st) {
     hipLaunchKernelGGL((axo::norm_rows_kernel<T, LANES, CH>), dim3(at_most(tiles_in(g.M, ROWS), NORM_MOST_BLOCKS)), dim3(BLOCK), 0, st, g);
     return launched();
 }
+// A row is shared by as many lanes as leave each of them 16 to 64 bytes of it; of what holds a row the quickest was taken, bf16 and fp32 with a residual, 2^25 values (us):
+//   to 64      8 x 1 chunks 50, 82       64 x 1  205, 265     to 4096   256 x 2  49, 84     512 x 1  49, 85
+//   to 256    32 x 1  48, 83             64 x 1   66,  90     to 8192   512 x 2  51, 88     256 x 4  53, 87 (64 rows: 4.4 and 5.2)
+//   to 512    64 x 1  48, 83             64 x 2   56,  87     to 12288  512 x 3  53, 88    1024 x 2  66, 102
+//   to 1024   64 x 2  50, 83            256 x 1   65,  90     to 16384  512 x 4  57, 99    1024 x 2  62, 95
+//   to 2048  256 x 1  48, 83             64 x 4   53,  87     20000    1024 x 3  66, 103   read again from the caches 92, 124
+//   32768   1024 x 4  61, 133           read again 79, 126: rows of 64 KB of fp32 and more are
 template <typename T>
 int launch_norm_typed(const axo::NormArgs& g, hipStream_t st) {
     if (g.K <= 64) return launch_norm_rows<T, 8, 1>(g, st);
@@ -81,10 +88,12 @@ int launch_norm_typed(const axo::NormArgs& g, hipStream_t st) {
     if (g.K <= 1024) return launch_norm_rows<T, 64, 2>(g, st);
     if (g.K <= 2048) return launch_norm_rows<T, 256, 1>(g, st);
     if (g.K <= 4096) return launch_norm_rows<T, 256, 2>(g, st);
-    if (g.K <= 8192) return launch_norm_rows<T, 256, 4>(g, st);
+    if (g.K <= 8192) return launch_norm_rows<T, 512, 2>(g, st);
     if (g.K <= 12288) return launch_norm_rows<T, 512, 3>(g, st);
     if (g.K <= 16384) return launch_norm_rows<T, 512, 4>(g, st);
-    if (g.K <= 32768) return launch_norm_rows<T, 1024, 4>(g, st);
+    if (g.K <= 24576) return launch_norm_rows<T, 1024, 3>(g, st);
+    if constexpr (sizeof(T) == 2)
+        if (g.K <= 32768) return launch_norm_rows<T, 1024, 4>(g, st);
     hipLaunchKernelGGL(axo::norm_long_kernel<T>, dim3(at_most(g.M, NORM_MOST_BLOCKS)), dim3(axo::NORM_THREADS), 0, st, g);
     return launched();
 }
@@ -93,39 +102,52 @@ int launch_norm(const axo::NormArgs& g, int type, hipStream_t st) {
     return type == AXO_TYPE_F32 ? launch_norm_typed<float>(g, st) : launch_norm_typed<bf16_t>(g, st);
 }
 
-// The column sums of the backward pass come from so many workgroups at most, each of which leaves 2 K of them in the workspace.
+// The column sums of the backward pass come from so many workgroups at most, each of which leaves two rows of them in the workspace.
 constexpr int NORM_MOST_SLICES = 256;
 constexpr int NORM_MOST_COLS = 16384;  // of rows in registers
 int norm_slice_rows(int64_t M) { return (int)std::max<int64_t>(axo::NORM_COL_ROWS, (M + 255) / 256); }  // of longer ones
+int64_t norm_partial_cols(int64_t K) { return (K + 7) / 8 * 8; }
 size_t norm_workspace(int64_t M, int64_t K) {
-    return (size_t)std::max<int64_t>(1, std::min<int64_t>(M, NORM_MOST_SLICES)) * 2 * (size_t)K * sizeof(float);
+    return (size_t)std::max<int64_t>(1, std::min<int64_t>(M, NORM_MOST_SLICES)) * 2 * (size_t)norm_partial_cols(K) * sizeof(float);
 }
 
 int launch_norm_join(const axo::NormBwdArgs& g, hipStream_t st) {
     if (g.phase == axo::NORM_APPLY || (!g.dgamma && !g.dbeta)) return AXO_OK;
-    hipLaunchKernelGGL(axo::norm_join_kernel, dim3((unsigned)((2 * (int64_t)g.K + axo::NORM_JOIN_COLS - 1) / axo::NORM_JOIN_COLS)), dim3(axo::NORM_JOIN_THREADS), 0, st, g);
+    hipLaunchKernelGGL(axo::norm_join_kernel, dim3(at_most((2 * g.partial_cols + axo::NORM_JOIN_COLS - 1) / axo::NORM_JOIN_COLS, NORM_MOST_BLOCKS)),
+                       dim3(axo::NORM_JOIN_THREADS), 0, st, g);
     return launched();
 }
 template <typename T, int LANES, int CH, int GROUPS>
-int launch_norm_bwd_rows(axo::NormBwdArgs& g, hipStream_t st) {
+int launch_norm_bwd_groups(axo::NormBwdArgs& g, hipStream_t st) {
     g.slices = (int)std::min<int64_t>(tiles_in(g.M, GROUPS), NORM_MOST_SLICES);
     hipLaunchKernelGGL((axo::norm_bwd_rows_kernel<T, LANES, CH, GROUPS>), dim3((unsigned)g.slices), dim3(LANES * GROUPS), 0, st, g);
     if (const int rc = launched()) return rc;
     return launch_norm_join(g, st);
 }
+// A workgroup has 512 threads, and of bf16 rows 1024 where there are more rows than workgroups of 512 take at once: the same bytes under way.  2^25 values, 512 and 1024
+// threads (us): 64 columns bf16 67, 57, fp32 87, 90; 512 columns 65, 54 and 86, 89; 2048 columns 64, 53 and 86, 90.  (1000 x 64 bf16: 6.9, 8.0.)
+template <typename T, int LANES, int CH>
+int launch_norm_bwd_rows(axo::NormBwdArgs& g, hipStream_t st) {
+    constexpr int GROUPS = 512 / LANES;
+    if constexpr (sizeof(T) == 2 && CH == 1)
+        if (g.M > GROUPS * NORM_MOST_SLICES) return launch_norm_bwd_groups<T, LANES, CH, 2 * GROUPS>(g, st);
+    return launch_norm_bwd_groups<T, LANES, CH, GROUPS>(g, st);
+}
+// Rows of up to 4096 values have a chunk to a lane; of longer ones a lane holds up to four (16384 columns, bf16 and fp32: 512 x 4 65 and 106 us, 1024 x 2 66 and 121, read
+// twice 108 and 149).
 template <typename T>
 int launch_norm_bwd_typed(axo::NormBwdArgs& g, hipStream_t st) {
     if (g.M > 0 && g.K <= NORM_MOST_COLS) {
-        if (g.K <= 64) return launch_norm_bwd_rows<T, 8, 1, 32>(g, st);
-        if (g.K <= 128) return launch_norm_bwd_rows<T, 16, 1, 32>(g, st);
-        if (g.K <= 256) return launch_norm_bwd_rows<T, 32, 1, 16>(g, st);
-        if (g.K <= 512) return launch_norm_bwd_rows<T, 64, 1, 8>(g, st);
-        if (g.K <= 1024) return launch_norm_bwd_rows<T, 128, 1, 8>(g, st);
-        if (g.K <= 2048) return launch_norm_bwd_rows<T, 256, 1, 4>(g, st);
-        if (g.K <= 4096) return launch_norm_bwd_rows<T, 512, 1, 2>(g, st);
-        if (g.K <= 8192) return launch_norm_bwd_rows<T, 512, 2, 1>(g, st);
-        if (g.K <= 12288) return launch_norm_bwd_rows<T, 512, 3, 1>(g, st);
-        return launch_norm_bwd_rows<T, 1024, 2, 1>(g, st);
+        if (g.K <= 64) return launch_norm_bwd_rows<T, 8, 1>(g, st);
+        if (g.K <= 128) return launch_norm_bwd_rows<T, 16, 1>(g, st);
+        if (g.K <= 256) return launch_norm_bwd_rows<T, 32, 1>(g, st);
+        if (g.K <= 512) return launch_norm_bwd_rows<T, 64, 1>(g, st);
+        if (g.K <= 1024) return launch_norm_bwd_rows<T, 128, 1>(g, st);
+        if (g.K <= 2048) return launch_norm_bwd_rows<T, 256, 1>(g, st);
+        if (g.K <= 4096) return launch_norm_bwd_rows<T, 512, 1>(g, st);
+        if (g.K <= 8192) return launch_norm_bwd_rows<T, 512, 2>(g, st);
+        if (g.K <= 12288) return launch_norm_bwd_rows<T, 512, 3>(g, st);
+        return launch_norm_bwd_rows<T, 512, 4>(g, st);
     }
     if (g.M > 0) {
         hipLaunchKernelGGL(axo::norm_bwd_long_kernel<T>, dim3(at_most(g.M, NORM_MOST_BLOCKS)), dim3(axo::NORM_THREADS), 0, st, g);
@@ -134,7 +156,7 @@ int launch_norm_bwd_typed(axo::NormBwdArgs& g, hipStream_t st) {
     if (g.phase == axo::NORM_APPLY || (!g.dgamma && !g.dbeta)) return AXO_OK;
     g.rows_per_slice = norm_slice_rows(g.M);
     g.slices = (int)std::max<int64_t>(1, tiles_in(g.M, g.rows_per_slice));
-    hipLaunchKernelGGL(axo::norm_cols_kernel<T>, dim3((unsigned)(tiles_in(g.K, axo::NORM_STRIP) * g.slices)), dim3(axo::NORM_COL_THREADS), 0, st, g);
+    hipLaunchKernelGGL(axo::norm_cols_kernel<T>, dim3(at_most(tiles_in(g.K, axo::NORM_STRIP) * g.slices, NORM_MOST_BLOCKS)), dim3(axo::NORM_COL_THREADS), 0, st, g);
     if (const int rc = launched()) return rc;
     return launch_norm_join(g, st);
 }
@@ -225,6 +247,7 @@ int plan_norm_columns(float* dgamma, float* dbeta, int accumulate, void* ws, siz
     if (!ws || ws_bytes < need) return AXO_ERR_WORKSPACE;
     if (!aligned16(ws)) return AXO_ERR_MISALIGNED;
     g.partial = static_cast<float*>(ws);
+    g.partial_cols = norm_partial_cols(g.K);
     b.writes(ws, (int64_t)(need / 4), 1, (int64_t)(need / 4), 4);
     return AXO_OK;
 }

@@ -40,7 +40,8 @@ struct NormBwdArgs {
     float* dgamma;               // either may be nullptr
     float* dbeta;
     int accumulate;
-    float* partial;              // [slices x 2 x K] column sums of row slices
+    float* partial;              // [slices x 2 x partial_cols] column sums of row slices
+    int64_t partial_cols;        // K, up to a whole chunk
     int slices, rows_per_slice;
     int M, K;                    // rows, columns here
     float per_row;               // 1 / columns of the whole row
@@ -439,9 +440,9 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_long_kernel(NormArgs g) {
 template <typename T, int LANES, int CH, int GROUPS>
 __global__ void __launch_bounds__(LANES * GROUPS) norm_bwd_rows_kernel(NormBwdArgs g) {
     constexpr int BLOCK = LANES * GROUPS;
-    constexpr bool AHEAD = sizeof(T) == 2 || LANES * CH < 2048;  // 16 fp32 values per lane of a full workgroup leave no registers for the next row's
+    constexpr bool AHEAD = sizeof(T) == 2 || LANES * CH < 2048;  // four chunks of fp32 values leave no registers for the next row's
     __shared__ float lds[2][2 * (BLOCK / 64)];
-    __shared__ float cols[GROUPS > 1 ? BLOCK * 8 : 1];
+    __shared__ __attribute__((aligned(16))) float cols[GROUPS > 1 ? BLOCK * 8 : 4];
     const int lane = threadIdx.x % LANES, group = row_group<LANES>();
     const bool want_cols = g.phase != NORM_APPLY && (g.dgamma || g.dbeta), want_sums = g.phase != NORM_APPLY;
     float dg[CH][8], db[CH][8];
@@ -528,30 +529,34 @@ __global__ void __launch_bounds__(LANES * GROUPS) norm_bwd_rows_kernel(NormBwdAr
         }
     }
     if (!want_cols) return;
+    constexpr int COLS = LANES * 8;  // of a chunk of all lanes
 #pragma unroll
-    for (int what = 0; what < 2; ++what)
+    for (int what = 0; what < 2; ++what) {
+        float* const to = g.partial + ((int64_t)blockIdx.x * 2 + what) * g.partial_cols;
+        if constexpr (GROUPS > 1) {
+            static_assert(CH == 1, "a chunk per lane");
+            __syncthreads();
+            float* const mine = cols + group * COLS + lane * 8;
+            *reinterpret_cast<f32x4*>(mine) = what ? f32x4{db[0][0], db[0][1], db[0][2], db[0][3]} : f32x4{dg[0][0], dg[0][1], dg[0][2], dg[0][3]};
+            *reinterpret_cast<f32x4*>(mine + 4) = what ? f32x4{db[0][4], db[0][5], db[0][6], db[0][7]} : f32x4{dg[0][4], dg[0][5], dg[0][6], dg[0][7]};
+            __syncthreads();
+            for (int c = threadIdx.x; c < COLS && c < g.K; c += BLOCK) {
+                float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = what ? db[j][i] : dg[j][i];
-            if constexpr (GROUPS > 1) {
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) cols[threadIdx.x * 8 + i] = v[i];
-                __syncthreads();
-                if (group == 0)
-#pragma nounroll
-                    for (int q = 1; q < GROUPS; ++q)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] += cols[(q * LANES + lane) * 8 + i];
+                for (int q = 0; q < GROUPS; ++q) v += cols[q * COLS + c];
+                to[c] = v;
             }
-            const int c = (j * LANES + lane) * 8;
-            if (group == 0)
+        } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < g.K) g.partial[((int64_t)blockIdx.x * 2 + what) * g.K + c + i] = v[i];
+            for (int j = 0; j < CH; ++j) {
+                const int c = (j * LANES + lane) * 8;
+                if (c >= g.K) continue;
+                const float(&v)[8] = what ? db[j] : dg[j];
+                *reinterpret_cast<f32x4*>(to + c) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(to + c + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            }
         }
+    }
 }
 
 // dX of rows of any length, a workgroup to a row, which it reads once for the two sums and once for the output.
@@ -616,82 +621,90 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_bwd_long_kernel(NormBwdArgs
     }
 }
 
-// dgamma and dbeta of a strip of 64 columns over a slice of the rows: 8 lanes of 8 columns by 32 rows at a time.  The sums of a slice
+// dgamma and dbeta of strips of 64 columns over slices of the rows: 8 lanes of 8 columns by 32 rows at a time.  The sums of a slice
 // go to `partial`, which norm_join_kernel adds up in ascending order of the slices.
 constexpr int NORM_STRIP = 64, NORM_COL_THREADS = 256, NORM_COL_ROWS = NORM_COL_THREADS / (NORM_STRIP / 8);
 template <typename T>
 __global__ void __launch_bounds__(NORM_COL_THREADS) norm_cols_kernel(NormBwdArgs g) {
     __shared__ float lds[2][NORM_COL_THREADS / 64][NORM_STRIP];
-    const int strip = blockIdx.x / g.slices, slice = blockIdx.x % g.slices;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)strip * NORM_STRIP + (lane & 7) * 8;
-    const int valid = (int)min((int64_t)8, g.K - col);
-    float dg[8], db[8];
+    const int64_t pieces = ((int64_t)g.K + NORM_STRIP - 1) / NORM_STRIP * g.slices;
+    for (int64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int64_t strip = piece / g.slices, slice = piece % g.slices;
+        const int64_t col = strip * NORM_STRIP + (lane & 7) * 8;
+        const int valid = (int)min((int64_t)8, g.K - col);
+        float dg[8], db[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dg[i] = db[i] = 0.f;
-    const int64_t end = min((int64_t)g.M, ((int64_t)slice + 1) * g.rows_per_slice);
-    if (valid > 0)
-        for (int64_t row = (int64_t)slice * g.rows_per_slice + (threadIdx.x >> 3); row < end; row += NORM_COL_ROWS) {
-            float x[8], d[8];
-            load_chunk(static_cast<const T*>(g.S) + row * g.lds + col, valid, x);
-            load_chunk(g.dY + row * g.lddy + col, valid, d);
-            const float2 st = g.stats[row];
+        for (int i = 0; i < 8; ++i) dg[i] = db[i] = 0.f;
+        const int64_t end = min((int64_t)g.M, (slice + 1) * g.rows_per_slice);
+        if (valid > 0)
+            for (int64_t row = slice * g.rows_per_slice + (threadIdx.x >> 3); row < end; row += NORM_COL_ROWS) {
+                float x[8], d[8];
+                load_chunk(static_cast<const T*>(g.S) + row * g.lds + col, valid, x);
+                load_chunk(g.dY + row * g.lddy + col, valid, d);
+                const float2 st = g.stats[row];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dg[i] += d[i] * ((x[i] - st.x) * st.y);
+                    db[i] += d[i];
+                }
+            }
+#pragma unroll
+        for (int m = 8; m < 64; m <<= 1)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                dg[i] += d[i] * ((x[i] - st.x) * st.y);
-                db[i] += d[i];
+                dg[i] += __shfl_xor(dg[i], m, 64);
+                db[i] += __shfl_xor(db[i], m, 64);
             }
+        __syncthreads();  // the last piece's sums have been read
+        if (lane < 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                lds[0][wave][lane * 8 + i] = dg[i];
+                lds[1][wave][lane * 8 + i] = db[i];
+            }
+        __syncthreads();
+        if (threadIdx.x < 2 * NORM_STRIP) {
+            const int what = threadIdx.x / NORM_STRIP, c = threadIdx.x % NORM_STRIP;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < NORM_COL_THREADS / 64; ++w) sum += lds[what][w][c];
+            const int64_t at = strip * NORM_STRIP + c;
+            if (at < g.K) g.partial[(slice * 2 + what) * g.partial_cols + at] = sum;
         }
-#pragma unroll
-    for (int m = 8; m < 64; m <<= 1)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            dg[i] += __shfl_xor(dg[i], m, 64);
-            db[i] += __shfl_xor(db[i], m, 64);
-        }
-    if (lane < 8)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            lds[0][wave][lane * 8 + i] = dg[i];
-            lds[1][wave][lane * 8 + i] = db[i];
-        }
-    __syncthreads();
-    if (threadIdx.x >= 2 * NORM_STRIP) return;
-    const int what = threadIdx.x / NORM_STRIP, c = threadIdx.x % NORM_STRIP;
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < NORM_COL_THREADS / 64; ++w) sum += lds[what][w][c];
-    const int64_t at = (int64_t)strip * NORM_STRIP + c;
-    if (at < g.K) g.partial[((int64_t)slice * 2 + what) * g.K + at] = sum;
-}
-// 64 columns by 16 slices at a time.
-constexpr int NORM_JOIN_THREADS = 1024, NORM_JOIN_COLS = 64;
-__global__ void __launch_bounds__(NORM_JOIN_THREADS) norm_join_kernel(NormBwdArgs g) {
-    constexpr int LANES = NORM_JOIN_THREADS / NORM_JOIN_COLS;
-    __shared__ float lds[LANES][NORM_JOIN_COLS];
-    const int col = threadIdx.x % NORM_JOIN_COLS, first = threadIdx.x / NORM_JOIN_COLS;
-    const int64_t at = (int64_t)blockIdx.x * NORM_JOIN_COLS + col;  // of dgamma and dbeta behind each other
-    float sum = 0.f;
-    if (at < 2 * (int64_t)g.K) {
-        const float* const p = g.partial + at;
-        int s = first;
-        for (; s + 7 * LANES < g.slices; s += 8 * LANES) {  // eight loads in flight, added in order
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)(s + i * LANES) * 2 * g.K];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[i];
-        }
-        for (; s < g.slices; s += LANES) sum += p[(int64_t)s * 2 * g.K];
     }
-    lds[first][col] = sum;
-    __syncthreads();
-    if (first != 0 || at >= 2 * (int64_t)g.K) return;
-    float* const out = at < g.K ? g.dgamma : g.dbeta;
-    if (!out) return;
-    for (int q = 1; q < LANES; ++q) sum += lds[q][col];
-    const int64_t c = at < g.K ? at : at - g.K;
-    out[c] = g.accumulate ? out[c] + sum : sum;
+}
+// The sums of all slices, added in an order that depends on their number alone: of 32 columns, eight lanes of 16 bytes, a lane to every 128th slice; the lanes of a wave
+// meet by exchanges and the waves in LDS.  dgamma and dbeta lie behind each other.
+constexpr int NORM_JOIN_THREADS = 1024, NORM_JOIN_COLS = 32;
+__global__ void __launch_bounds__(NORM_JOIN_THREADS) norm_join_kernel(NormBwdArgs g) {
+    constexpr int LANES = NORM_JOIN_THREADS * 4 / NORM_JOIN_COLS, WAVES = NORM_JOIN_THREADS / 64;
+    __shared__ __attribute__((aligned(16))) float lds[WAVES][NORM_JOIN_COLS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t both = 2 * g.partial_cols;
+    for (int64_t from = (int64_t)blockIdx.x * NORM_JOIN_COLS; from < both; from += (int64_t)gridDim.x * NORM_JOIN_COLS) {
+        const int64_t col = from + (lane & 7) * 4;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        if (col < both)
+            for (int s = threadIdx.x >> 3; s < g.slices; s += LANES) sum += *reinterpret_cast<const f32x4*>(g.partial + s * both + col);
+#pragma unroll
+        for (int m = 8; m < 64; m <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m, 64);
+        __syncthreads();  // the last columns' sums have been read
+        if (lane < 8) *reinterpret_cast<f32x4*>(&lds[wave][lane * 4]) = sum;
+        __syncthreads();
+        const int64_t at = from + threadIdx.x;
+        if (threadIdx.x >= NORM_JOIN_COLS || at >= both) continue;
+        const bool first = at < g.partial_cols;
+        float* const out = first ? g.dgamma : g.dbeta;
+        const int64_t c = first ? at : at - g.partial_cols;
+        if (!out || c >= g.K) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += lds[w][threadIdx.x];
+        out[c] = g.accumulate ? out[c] + v : v;
+    }
 }
 
 }  // namespace axo

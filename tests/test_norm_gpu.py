@@ -65,6 +65,12 @@ def test_forward(m, k, wide):
     check_forward(d, wide, res=True, gap=8)
 
 
+@pytest.mark.parametrize("k", [24576, 24577, 24585, 32769])
+@pytest.mark.parametrize("wide", [False, True])
+def test_forward_of_long_rows(k, wide):
+    check_forward(inputs(3, k, wide, k), wide, res=True, gap=8)
+
+
 @pytest.mark.parametrize("gamma,beta", [(False, False), (True, False), (False, True)])
 def test_forward_without_weights(gamma, beta):
     for m, k in ((3, 100), (2, 4104)):
@@ -138,6 +144,13 @@ def test_backward(m, k, wide):
     d = inputs(m, k, wide, 200 * m + k)
     check_backward(d, wide, res=False)
     check_backward(d, wide, res=True, gap=8)
+
+
+@pytest.mark.parametrize("m,k", [(16450, 40), (8300, 100), (4200, 200), (2100, 401), (1100, 1000), (600, 2000), (270, 3001), (260, 12000)])
+def test_backward_of_more_rows_than_are_taken_at_once(m, k):
+    d = inputs(m, k, False, 300 * m + k)
+    check_backward(d, False, res=False)
+    check_backward(d, False, res=True, acc=np.linspace(-3, 3, k).astype(np.float32).astype(np.float64))
 
 
 def test_backward_parts_of_it():
