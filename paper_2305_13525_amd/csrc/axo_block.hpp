@@ -271,11 +271,13 @@ bool gated_spans_ok(const GatedArgs& g) {
     return fits(256 * g.lda + walked) && fits(OP == axo::GATED_FWD ? walked * g.ldb + 256 : 256 * g.ldb + walked);
 }
 
-// Rows of the outputs that straddle cache lines are stored plainly (store_row).
+// Rows of the outputs that straddle cache lines are stored plainly (store_row), but past the caches where the forward pass writes more than they keep for
+// a line's other half: whole lines 4096 x 2048 x 4096 through the activation's derivative 73 us plainly and 64 past the caches; straddled 4096 x 2048 x 12296 247 and 271; forward,
+// G and U kept, straddled 2048 x 2048 x 6008 87 and 95, 4096 x 2048 x 8200 271 and 241.
 template <int OP>
 bool gated_plain(const GatedArgs& g) {
-    auto straddles = [](const void* p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 2)) & 127) != 0; };
-    return straddles(g.C, g.ldc);
+    const bool straddles = ((reinterpret_cast<uintptr_t>(g.C) | (uintptr_t)(g.ldc * 2)) & 127) != 0;
+    return straddles && (OP != axo::GATED_FWD || (int64_t)g.Mo * g.No * (g.G ? 6 : 2) <= (int64_t)128 << 20);
 }
 
 template <typename C, int OP, typename Kernel>
@@ -304,7 +306,7 @@ int launch_gated_on(const GatedArgs& g, Tiles tiles, const axo::TileSched& sc, h
     return launched();
 }
 // On the tiles of a plan.  Where rows of the inputs are fetched by whole lines those of the outputs mostly straddle lines as well, so there is one kind of
-// such kernels, with plain stores.  dX, whose two products may lie differently in their lines, does not do that, and its epilogue looks at the output itself.
+// such kernels, with plain stores, and forward one more.  dX, whose two products may lie differently in their lines, does not do that, and its epilogue looks at the output itself.
 template <int OP>
 int launch_gated_tiles_of(const GatedArgs& g, Tiles tiles, int cols, int red, hipStream_t st) {
     const axo::TileSched sc = tiles == Tiles::big ? plan_columns(g.Mo, cols, red) : axo::TileSched{};
@@ -314,7 +316,10 @@ int launch_gated_tiles_of(const GatedArgs& g, Tiles tiles, int cols, int red, hi
         as_one.No = cols;
         switch (takes_lines_on(as_one, axo::KC, axo::GATED_LB<OP>, tiles, sc)) {
             case 2: return launch_gated_on<OP, true, 2>(g, tiles, sc, st);
-            case 1: return launch_gated_on<OP, true, 1>(g, tiles, sc, st);
+            case 1:
+                if constexpr (OP == axo::GATED_FWD)
+                    if (!gated_plain<OP>(g)) return launch_gated_on<OP, false, 1>(g, tiles, sc, st);
+                return launch_gated_on<OP, true, 1>(g, tiles, sc, st);
             default: break;
         }
         return gated_plain<OP>(g) ? launch_gated_on<OP, true, 0>(g, tiles, sc, st) : launch_gated_on<OP, false, 0>(g, tiles, sc, st);
