@@ -79,6 +79,7 @@ VARIANTS = [
     (0, 16, 128, False, (1, 3328, 16608)), (0, 16, 128, True, (1, 4618, 10914)),
     (0, 32, 32, False, (290, 1280, 8)), (0, 32, 32, False, (268, 975, 10)), (0, 32, 32, True, (321, 2304, 8)), (0, 32, 32, True, (270, 2004, 10)),
     (0, 64, 32, False, (1, 64, 8)), (0, 64, 32, False, (1, 8, 9)), (0, 64, 64, False, (3, 1024, 14565)), (0, 64, 64, False, (1, 964, 14028)),
+    (0, 64, 64, False, (130, 256, 4200)), (0, 64, 64, False, (140, 250, 4203)), (1, 64, 128, False, (130, 640, 8300)), (1, 64, 128, False, (135, 643, 8303)),
     (0, 128, 64, False, (17, 64, 8880)), (0, 128, 64, False, (20, 8, 8199)), (0, 256, 128, False, (133, 64, 9416)), (0, 256, 128, False, (137, 8, 9259)),
     (1, 16, 32, False, (2, 1920, 8)), (1, 16, 32, False, (1, 1840, 9)), (1, 16, 32, True, (1, 2048, 8)), (1, 16, 32, True, (2, 2016, 9)),
     (1, 32, 32, False, (1, 768, 8)), (1, 32, 32, False, (1, 705, 9)), (1, 32, 32, True, (351, 2112, 8)), (1, 32, 32, True, (258, 2073, 9)),
