@@ -419,14 +419,19 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     plan.tiles = quickest_tiles(Mo, (int)cols, (int)red);
     const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);
     const double tiles_us = std::max(tiles_time(plan.tiles, Mo, (int)cols, (int)red) * GATED_TILES[OP][(int)plan.tiles], 3.0 + weights / 5.0);
+    const int64_t small_tiles = tiles_in(Mo, 64) * tiles_in((int)cols, 64);
     const bool round_of_wide = tiles_in(Mo, 64) * tiles_in((int)cols, 128) <= NUM_CU;
     if (plan.tiles == Tiles::tall) plan.tiles = round_of_wide ? Tiles::wide : Tiles::mid;
     // 64 x 64 tiles that leave some CUs two and others one: a 64 x 128 tile for each CU is quicker, from four steps of a reduction on forward and from ten through the
     // activation's derivative, where G and U of a tile wait for its end.  Of 55 such shapes where 64 x 64 tiles were taken, forward 5 to 56 % over four steps (350 x 5928 x 1453 55 us
     // and 37, 1001 x 1027 x 515 12.1 and 10.1) and 0 to -5 % at two; backward 2 to 14 % from ten steps on (700 x 4000 x 1500 26.0 and 22.9), -10 to 3 % below.
-    if (OP != axo::GATED_DX && plan.tiles == Tiles::small && round_of_wide && tiles_in(Mo, 64) * tiles_in((int)cols, 64) > NUM_CU &&
-        steps_in(R) >= (OP == axo::GATED_FWD ? 4 : 10))
-        plan.tiles = Tiles::wide;
+    if (OP != axo::GATED_DX && plan.tiles == Tiles::small && round_of_wide && small_tiles > NUM_CU && steps_in(R) >= (OP == axo::GATED_FWD ? 4 : 10)) plan.tiles = Tiles::wide;
+    // Short reductions through the derivative are its reads of G and U and its stores, which go on beside each other where a CU has two tiles: 64 x 64 ones,
+    // while there are few of them.  Of 126 shapes with reductions of 32 to 1024: for 128 x 128 tiles, to four steps and two a CU, 42 to 51 % quicker (2638 x 32 x 640 8.6 us and 6.0);
+    // for 256 x 256 ones to nine a CU and four steps 0 to 50 % (876 x 192 x 8576 28.6 and 19.1), to six and sixteen steps -1 to 28 %; beyond, 11 % quicker to 27 % slower.
+    if (OP == axo::GATED_DACT && ((plan.tiles == Tiles::mid && R <= 256 && small_tiles <= 2 * NUM_CU) ||
+                                  (plan.tiles == Tiles::big && R <= 1024 && small_tiles <= (R <= 256 ? 9 : 6) * NUM_CU)))
+        plan.tiles = Tiles::small;
     if (Mo > 2048) return plan;  // never quicker there
     double us;
     const GatedCut cut = gated_cut<OP>(Mo, No, R, &us);

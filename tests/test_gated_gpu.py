@@ -84,7 +84,8 @@ VARIANTS = [
     (1, 16, 32, False, (2, 1920, 8)), (1, 16, 32, False, (1, 1840, 9)), (1, 16, 32, True, (1, 2048, 8)), (1, 16, 32, True, (2, 2016, 9)),
     (1, 32, 32, False, (1, 768, 8)), (1, 32, 32, False, (1, 705, 9)), (1, 32, 32, True, (351, 2112, 8)), (1, 32, 32, True, (258, 2073, 9)),
     (1, 64, 64, False, (1, 64, 8)), (1, 64, 64, False, (1, 8, 9)), (1, 64, 128, False, (23, 1088, 19000)), (1, 64, 128, False, (20, 961, 18788)),
-    (1, 128, 128, False, (21, 64, 17144)), (1, 128, 128, False, (19, 8, 16533)), (1, 256, 256, False, (144, 64, 16512)), (1, 256, 256, False, (129, 8, 17245)),
+    (1, 128, 128, False, (330, 64, 6000)), (1, 128, 128, False, (325, 8, 6007)), (1, 256, 256, False, (700, 64, 13824)), (1, 256, 256, False, (697, 8, 13801)),
+    (1, 64, 64, False, (21, 64, 17144)), (1, 64, 64, False, (19, 8, 16533)), (1, 64, 64, False, (144, 64, 16512)), (1, 64, 64, False, (129, 8, 17245)),
     (2, 16, 32, False, (2, 64, 840)), (2, 16, 32, False, (1, 9, 806)), (2, 16, 32, True, (1, 64, 968)), (2, 16, 32, True, (1, 9, 961)),
     (2, 32, 32, False, (1, 64, 360)), (2, 32, 32, False, (2, 9, 354)), (2, 32, 32, True, (294, 64, 992)), (2, 32, 32, True, (272, 10, 962)),
     (2, 64, 64, False, (1, 64, 8)), (2, 64, 64, False, (1, 9, 8)), (2, 64, 128, False, (3904, 320, 504)), (2, 64, 128, False, (3678, 282, 481)),
