@@ -8,6 +8,8 @@
 // Slices: a workgroup writes its fp32 sums to the workspace and counts itself in on its tile's counter; whoever comes last adds the slices in
 // ascending order and finishes the tile, and sets the counter back to zero.  Which workgroup that is depends on timing, what it computes does not.
 // All of that goes past the L2 of an XCD by device-scope accesses, without fences (as bias_grad_split_kernel).
+// Measured, weights from memory: forward 1 x 8192 x 16384 99 us, 5.4 TB/s (a large copy 4.8, a stream of reads alone 5.8); dX of 96 x 2048 x 6144 20 us, 2.5 TB/s, its weights read once
+// from memory and by three tiles from the caches.  On the tiles of gemm_tile.hpp these take 104 and 34.
 #pragma once
 #include "gate.hpp"
 #include "gemm_slim.hpp"

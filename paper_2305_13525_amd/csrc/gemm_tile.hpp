@@ -928,7 +928,7 @@ __device__ __forceinline__ void store_eight(const u32x4 v, bf16_t* to, const boo
 
 // Forward: a wave's first TN / 2 blocks of 16 columns are those of G, the others the same columns of U, so H is formed in registers.  A
 // wave has only half of a 128-byte line of a row of H, so the whole tile is staged in LDS and stored by rows of the tile; G and U, where they are wanted,
-// go the same way in turn, through two regions.
+// go the same way in turn, through two regions.  (All three at once, where there is room: the same to one in a hundred, 4096 x 8192 x 16384 1.53 to 1.59 ms.)
 template <typename C, int BM, int BN, bool PLAIN, typename Args>
 __device__ __forceinline__ void gated_fwd_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int i0, const int j0, const int wm, const int wn,
                                                    const int tid, char* smem) {
@@ -991,7 +991,8 @@ __device__ __forceinline__ void gated_fwd_epilogue(const Args& g, f32x4 (&acc)[C
 }
 
 // Backward: dG = sum U act'(G), dU = sum act(G).  A wave stages its sums in fp32, 16 or 32 rows at a time, so that a lane then holds eight columns of a
-// row, reads G and U and stores both results 16 bytes at a time; what a pass reads is requested two passes ahead.
+// row, reads G and U and stores both results 16 bytes at a time; what a pass reads is requested two passes ahead.  (4096 x 8192 x 16384 839 us and 858 with
+// one pass ahead, 4000 x 2000 x 6000 140 and 147.  With every line of G and U touched ahead of the reduction 859 -> 885 and 139 -> 148: the loads that start it wait behind them.)
 template <typename C, bool PLAIN, typename Args>
 __device__ __forceinline__ void gated_dact_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int wrow0, const int wcol0, const int wave, const int lane,
                                                     char* smem, const bool whole) {
