@@ -127,7 +127,8 @@ int axo_gated_dgrad_act(const axo_problem_t *p, const void *dY, int64_t lddy, co
 int axo_gated_dgrad(const axo_problem_t *p, const void *dG, const void *dU, int64_t lddz, const void *Wg, const void *Wu, int64_t ldw,
                     void *dX, int64_t lddx, void *ws, size_t ws_bytes, void *hip_stream);
 
-/* dWg[Kl x Nl] = X^T . dG and dWu = X^T . dU, in one launch.  The bits of two axo_fc_wgrad. */
+/* dWg[Kl x Nl] = X^T . dG and dWu = X^T . dU, rounded once.  The bits of two axo_fc_wgrad, but where workgroups share a tile's reduction (many tokens and few
+ * outputs; axo_gated_tiles), which sum in another order, the same for every call. */
 int axo_gated_wgrad(const axo_problem_t *p, const void *X, int64_t ldx, const void *dG, const void *dU, int64_t lddz, void *dWg, void *dWu,
                     int64_t lddw, void *ws, size_t ws_bytes, void *hip_stream);
 
@@ -139,11 +140,12 @@ int axo_gated_wgrad_acc(const axo_problem_t *p, const void *X, int64_t ldx, cons
 size_t axo_gated_workspace_bytes(const axo_problem_t *p);
 
 /* The products of the block that have kernels of their own. */
-typedef enum axo_gated_op { AXO_GATED_OP_FWD = 0, AXO_GATED_OP_DGRAD_ACT = 1, AXO_GATED_OP_DGRAD = 2 } axo_gated_op_t;
+typedef enum axo_gated_op { AXO_GATED_OP_FWD = 0, AXO_GATED_OP_DGRAD_ACT = 1, AXO_GATED_OP_DGRAD = 2, AXO_GATED_OP_WGRAD = 3 } axo_gated_op_t;
 
 /* Host only.  How such a product is cut: rows and output columns of its tiles (of the largest, where there are two kinds), and the workgroups that share a
  * tile's reduction (1: one).  Rows of 16 and 32 are those of tiles whose waves split the reduction; 0 rows, with 0 columns and 0 slices: an empty output, or the
- * general kernel, which also takes operands whose spans pass 4 GiB, whatever is reported here.  A function of the shard's sizes alone, chosen by estimated time, so
+ * general kernel, which also takes operands whose spans pass 4 GiB, whatever is reported here.  For WGRAD 0 rows and columns and 1 slice: the tiles of
+ * axo_fc_wgrad.  A function of the shard's sizes alone, chosen by estimated time, so
  * that the answer may change from one version to the next.  Errors: those of axo_shard_dims; BAD_ARG (op); NULL_PTR. */
 int axo_gated_tiles(const axo_problem_t *p, int op, int *rows, int *cols, int *slices);
 

@@ -16,7 +16,7 @@ from .binding import (  # noqa: F401
     axo_shard_dims, axo_status_string, axo_version, axo_workspace_bytes, library, library_path,
 )
 from .block import (  # noqa: F401
-    AXO_GATE_GELU_ERF, AXO_GATE_GELU_TANH, AXO_GATE_SILU, AXO_GATED_OP_DGRAD, AXO_GATED_OP_DGRAD_ACT, AXO_GATED_OP_FWD, AXO_TYPE_BF16,
+    AXO_GATE_GELU_ERF, AXO_GATE_GELU_TANH, AXO_GATE_SILU, AXO_GATED_OP_DGRAD, AXO_GATED_OP_DGRAD_ACT, AXO_GATED_OP_FWD, AXO_GATED_OP_WGRAD, AXO_TYPE_BF16,
     AXO_TYPE_F32, axo_gated_act, axo_gated_dact, axo_gated_dgrad, axo_gated_dgrad_act, axo_gated_fwd, axo_gated_tiles, axo_gated_wgrad,
     axo_gated_wgrad_acc, axo_gated_workspace_bytes, axo_norm_apply, axo_norm_bwd,
     axo_norm_bwd_apply, axo_norm_bwd_part, axo_norm_fwd, axo_norm_part, axo_norm_workspace_bytes,

@@ -10,7 +10,7 @@ from .binding import Problem, _calls, _check, library
 
 AXO_TYPE_BF16, AXO_TYPE_F32 = 0, 1
 AXO_GATE_SILU, AXO_GATE_GELU_TANH, AXO_GATE_GELU_ERF = 0, 1, 2
-AXO_GATED_OP_FWD, AXO_GATED_OP_DGRAD_ACT, AXO_GATED_OP_DGRAD = 0, 1, 2
+AXO_GATED_OP_FWD, AXO_GATED_OP_DGRAD_ACT, AXO_GATED_OP_DGRAD, AXO_GATED_OP_WGRAD = 0, 1, 2, 3
 
 # kinds of arguments: p problem, v pointer, l int64_t, i int, f float, z size_t
 _SIGNATURES = {

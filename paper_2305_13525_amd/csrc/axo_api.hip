@@ -1289,6 +1289,14 @@ double tiles_time(Tiles tiles, int Mo, int No, int R) {
     }
 }
 
+double pair_time(int Mo, int No, int R, int la, int lb) {
+    GemmArgs g{};
+    g.Mo = Mo; g.No = No; g.R = R;
+    if (!prefers_slim(g, la, lb)) return tile_time(Mo, 2 * No, R);
+    const int pair = layout_pair(la, lb);
+    return std::min(slim_time(SLIM_MODEL[0], Mo, 2 * No, R, pair), slim_time(SLIM_MODEL[1], Mo, 2 * No, R, pair));
+}
+
 axo::TileSched plan_columns(int Mo, int No, int R) {
     axo::TileSched sc = plan_tiles(Mo, No);
     sc.shift = shift_units(Mo, No, R);

@@ -10,7 +10,7 @@
 #include "gated_slim.hpp"
 #include "norm.hpp"
 
-static_assert((int)AXO_GATED_OP_FWD == axo::GATED_FWD && (int)AXO_GATED_OP_DGRAD_ACT == axo::GATED_DACT && (int)AXO_GATED_OP_DGRAD == axo::GATED_DX, "one numbering");
+static_assert((int)AXO_GATED_OP_FWD == axo::GATED_FWD && (int)AXO_GATED_OP_DGRAD_ACT == axo::GATED_DACT && (int)AXO_GATED_OP_DGRAD == axo::GATED_DX && (int)AXO_GATED_OP_WGRAD == axo::GATED_DW, "one numbering");
 static_assert((int)AXO_GATE_SILU == axo::GATE_SILU && (int)AXO_GATE_GELU_TANH == axo::GATE_GELU_TANH && (int)AXO_GATE_GELU_ERF == axo::GATE_GELU_ERF, "one numbering");
 
 namespace axo_block {
@@ -362,6 +362,7 @@ struct GatedCut {
     int slices = 1, chunks = 0;
     size_t bytes = 0;  // of workspace
 };
+constexpr int GATED_SPLIT = 4;  // the kind of 128 x 128 tiles in slices
 // Slices of a reduction: as many as leave every workgroup a CU to itself and sixteen chunks, within 1 to 4 % of the best number over those shapes (two workgroups per CU: 3 to 9 %
 // off, eight chunks 3 to 7 %).
 int64_t gated_slices(int64_t tiles, int64_t chunks) { return std::max<int64_t>(1, std::min<int64_t>({NUM_CU / tiles, chunks / 16, 16})); }
@@ -398,6 +399,31 @@ GatedCut gated_cut(int Mo, int No, int R, double* us) {
     }
     return best;
 }
+// 128 x 128 tiles in the slices that are estimated to be quickest, all on the CUs at once, and the time of that: two launches, a slice's steps or the operands' way
+// from memory, and the sums' way through the workspace.  Taken where that is a fifth less than on whole tiles, or less than what gated_cut finds.  Of 160 drawn
+// products with a split, with and without it (us): forward 1760 x 15131 x 128 28 and 77, 128 x 11305 x 1778 25 and 54, through the derivative 512 x 10200 x 512 19 and 27, dX with the weight gradients
+// 128 x 2200 x 9344 51 and 80, 5784 x 640 x 752 42 and 115, 4413 x 3952 x 184 62 and 105; slower at worst by a quarter, where two slices of fewer than 20 steps looked better.
+template <int OP>
+GatedCut gated_split_cut(int Mo, int No, int R, double* us) {
+    GatedCut cut;
+    *us = 1e30;
+    const int64_t steps = steps_in(R), tm = tiles_in(Mo, 128), tn = tiles_in(No, axo::gated_cols<OP>(128)) * (OP == axo::GATED_DW ? 2 : 1), tiles = tm * tn;
+    for (int64_t asked = 2; asked <= 16 && asked * tiles <= NUM_CU; ++asked) {
+        const int64_t per = (steps + asked - 1) / asked, slices = (steps + per - 1) / per;
+        const double step = OP == axo::GATED_DX ? 0.9 : 0.45;
+        const double operands = 2e-6 * R * (OP == axo::GATED_DX ? 2.0 * Mo + 2.0 * No : Mo + (OP == axo::GATED_DACT ? 1.0 : 2.0) * No);  // MB
+        const double t = 8.5 + std::max(per * step, operands / 5.5) + 0.02 * (double)(tiles * slices);
+        if (per < 4 || t >= *us) continue;
+        *us = t;
+        cut.kind = GATED_SPLIT;
+        cut.tiles_m = tm;
+        cut.tiles_n = tn;
+        cut.slices = (int)slices;
+        cut.chunks = (int)per;
+        cut.bytes = GATED_COUNTER_BYTES + (size_t)(tiles * slices) * axo::SPLIT_TILE * sizeof(float);
+    }
+    return cut;
+}
 static_assert(NUM_CU <= GATED_MOST_TILES, "a counter for every tile that is sliced");
 
 // What a product of a gated block runs on, from its sizes alone.
@@ -432,10 +458,22 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     if (OP == axo::GATED_DACT && ((plan.tiles == Tiles::mid && R <= 256 && small_tiles <= 2 * NUM_CU) ||
                                   (plan.tiles == Tiles::big && R <= 1024 && small_tiles <= (R <= 256 ? 9 : 6) * NUM_CU)))
         plan.tiles = Tiles::small;
-    if (Mo > 2048) return plan;  // never quicker there
+    double us = 1e30, split_us;
+    GatedCut cut;
+    if (Mo <= 2048) cut = gated_cut<OP>(Mo, No, R, &us);  // never quicker beyond
+    const GatedCut split = gated_split_cut<OP>(Mo, No, R, &split_us);
+    if (split_us < std::min(us, 0.8 * tiles_us)) plan.cut = split;
+    else if (us < tiles_us) plan.cut = cut;
+    return plan;
+}
+
+// The same for the two weight gradients (K x N, M tokens), which are split or go the way of axo_fc_wgrad.
+GatedPlan gated_wgrad_plan(int K, int N, int M) {
+    GatedPlan plan;
+    if (K == 0 || N == 0 || M == 0 || N > INT32_MAX / 2) return plan;
     double us;
-    const GatedCut cut = gated_cut<OP>(Mo, No, R, &us);
-    if (us < tiles_us) plan.cut = cut;
+    const GatedCut split = gated_split_cut<axo::GATED_DW>(K, N, M, &us);
+    if (us < pair_time(K, N, M, axo::MC, axo::MC)) plan.cut = split;
     return plan;
 }
 
@@ -443,7 +481,7 @@ GatedPlan gated_plan(int Mo, int No, int R) {
 // plan takes a microsecond; a thread keeps those of the problems that it called last.
 struct GatedPlans {
     int64_t M = -1, K = -1, N = -1;
-    GatedPlan of[3];
+    GatedPlan of[4];
     size_t bytes = 0;
 };
 const GatedPlans& gated_plans(const Shard& s) {
@@ -454,7 +492,9 @@ const GatedPlans& gated_plans(const Shard& s) {
     p.of[axo::GATED_FWD] = gated_plan<axo::GATED_FWD>(M, N, K);
     p.of[axo::GATED_DACT] = gated_plan<axo::GATED_DACT>(M, K, N);
     p.of[axo::GATED_DX] = gated_plan<axo::GATED_DX>(M, K, N);
-    p.bytes = std::max({p.of[0].cut.bytes, p.of[1].cut.bytes, p.of[2].cut.bytes});
+    p.of[axo::GATED_DW] = gated_wgrad_plan(K, N, M);
+    p.bytes = 0;
+    for (const GatedPlan& plan : p.of) p.bytes = std::max(p.bytes, plan.cut.bytes);
     p.M = s.M;
     p.K = s.Kl;
     p.N = s.Nl;
@@ -481,6 +521,19 @@ int launch_gated_slim(const GatedArgs& g, const GatedCut& cut, void* ws, hipStre
         return launched();
     }
 }
+template <int OP, bool LINES>
+int launch_gated_split(const GatedArgs& g, const GatedCut& cut, void* ws, hipStream_t st) {
+    auto kern = axo::gated_split_kernel<OP, LINES>;
+    static std::atomic<uint64_t> raised{0};
+    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), axo::MidCfg::LDS_BYTES, &raised)) return AXO_ERR_HIP;
+    const int tiles = (int)(cut.tiles_m * cut.tiles_n);
+    const axo::GatedSplitSched sc{(int)cut.tiles_m, (int)cut.tiles_n, cut.slices, cut.chunks, reinterpret_cast<float*>(static_cast<char*>(ws) + GATED_COUNTER_BYTES)};
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * cut.slices)), dim3(axo::MidCfg::THREADS), axo::MidCfg::LDS_BYTES, st, axo::GatedProduct<OP>{g}, sc);
+    if (const int rc = launched()) return rc;
+    const int blocks = 128 * axo::gated_cols<OP>(128) / 4 / axo::SPLIT_JOIN_THREADS;
+    hipLaunchKernelGGL(axo::gated_split_join_kernel<OP>, dim3((unsigned)(tiles * blocks)), dim3(axo::SPLIT_JOIN_THREADS), 0, st, axo::GatedProduct<OP>{g}, sc);
+    return launched();
+}
 template <int OP>
 int launch_gated(const GatedArgs& g, const Shard& s, void* ws, hipStream_t st) {
     if (g.Mo == 0 || g.No == 0) return AXO_OK;
@@ -491,6 +544,13 @@ int launch_gated(const GatedArgs& g, const Shard& s, void* ws, hipStream_t st) {
         case 1: return launch_gated_slim<OP, 1>(g, plan.cut, ws, st);
         case 2: return launch_gated_slim<OP, 2>(g, plan.cut, ws, st);
         case 3: return launch_gated_slim<OP, 3>(g, plan.cut, ws, st);
+        case GATED_SPLIT:
+            if constexpr (OP != axo::GATED_DX) {
+                axo::GemmArgs as_one = g;
+                if (OP == axo::GATED_FWD) as_one.No *= 2;
+                if (takes_lines_on(as_one, axo::KC, axo::GATED_LB<OP>, Tiles::mid, {}) != 0) return launch_gated_split<OP, true>(g, plan.cut, ws, st);
+            }
+            return launch_gated_split<OP, false>(g, plan.cut, ws, st);
         default: break;
     }
     const int cols = OP == axo::GATED_FWD ? 2 * g.No : g.No, red = OP == axo::GATED_DX ? 2 * g.R : g.R;
@@ -535,6 +595,16 @@ int gated_wgrad(const axo_problem_t* p, const void* X, int64_t ldx, const void* 
     b.writes(dWg, lddw, s.Kl, s.Nl, sizeof(T));
     b.writes(dWu, lddw, s.Kl, s.Nl, sizeof(T));
     if (const int rc = first_error({check_gated_workspace(s, ws, ws_bytes, b), b.check()})) return rc;
+    if (const GatedCut& cut = gated_plans(s).of[axo::GATED_DW].cut; cut.kind == GATED_SPLIT) {
+        auto fits = [&](int64_t ld) { return (s.M + axo::TILE_BK) * ld * 2 + 256 < (int64_t)0xFFFF0000; };
+        GatedArgs h{};
+        h.A = static_cast<const bf16_t*>(X); h.lda = ldx;
+        h.B = static_cast<const bf16_t*>(dG); h.B2 = static_cast<const bf16_t*>(dU); h.ldb = lddz;
+        h.C = reinterpret_cast<bf16_t*>(dWg); h.U = reinterpret_cast<bf16_t*>(dWu); h.ldc = lddw;
+        h.Mo = (int)s.Kl; h.No = (int)s.Nl; h.R = (int)s.M;
+        h.epilogue = F32 ? axo::EPI_ACC_F32 : axo::EPI_NONE;
+        if (fits(ldx) && fits(lddz)) return launch_gated_split<axo::GATED_DW, false>(h, cut, ws, st);
+    }
     axo::GemmArgs g[2]{};
     for (int i = 0; i < 2; ++i) {
         g[i].A = static_cast<const bf16_t*>(X); g[i].lda = ldx;
@@ -816,13 +886,19 @@ int axo_gated_tiles(const axo_problem_t* p, int op, int* rows, int* cols, int* s
     return guarded([&]() -> int {
         Shard s;
         if (const int rc = derive_shard(p, &s)) return rc;
-        if (op < AXO_GATED_OP_FWD || op > AXO_GATED_OP_DGRAD) return AXO_ERR_BAD_ARG;
+        if (op < AXO_GATED_OP_FWD || op > AXO_GATED_OP_WGRAD) return AXO_ERR_BAD_ARG;
         if (!rows || !cols || !slices) return AXO_ERR_NULL_PTR;
         *rows = *cols = *slices = 0;
-        if (s.M == 0 || (op == AXO_GATED_OP_FWD ? s.Nl : s.Kl) == 0) return AXO_OK;
+        if (s.M == 0 || (op != AXO_GATED_OP_FWD && s.Kl == 0) || ((op == AXO_GATED_OP_FWD || op == AXO_GATED_OP_WGRAD) && s.Nl == 0)) return AXO_OK;
         const GatedPlan& plan = gated_plans(s).of[op];
         if (plan.general) return AXO_OK;
         *slices = plan.cut.slices;
+        if (plan.cut.kind == GATED_SPLIT) {
+            *rows = 128;
+            *cols = op == AXO_GATED_OP_FWD ? 64 : 128;
+            return AXO_OK;
+        }
+        if (op == AXO_GATED_OP_WGRAD) return AXO_OK;
         if (plan.cut.kind >= 0) {
             *rows = GATED_SLIM[op][plan.cut.kind].rows;
             *cols = GATED_SLIM[op][plan.cut.kind].cols;

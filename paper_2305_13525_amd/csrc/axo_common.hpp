@@ -33,11 +33,13 @@ enum Epilogue {
 //   GATED_FWD   two products with the same A in one tile, the columns of B and B2 beside each other; act(first) * second
 //   GATED_DACT  one product, taken through the derivative of that
 //   GATED_DX    the sum of two products, A B^T + A2 B2^T
-enum GatedOp { NOT_GATED = -1, GATED_FWD = 0, GATED_DACT = 1, GATED_DX = 2 };
+//   GATED_DW    one of two products with the same A (a tile like any other; split tiles know it)
+enum GatedOp { NOT_GATED = -1, GATED_FWD = 0, GATED_DACT = 1, GATED_DX = 2, GATED_DW = 3 };
 
 // One GEMM as the kernels see it.
 struct GemmArgs {
     static constexpr int OP = NOT_GATED;
+    static constexpr bool SPLIT = false;
     const bf16_t* A; int64_t lda;
     const bf16_t* B; int64_t ldb;
     bf16_t* C;       int64_t ldc;   // EPI_ACC_F32: C points to fp32 and ldc counts fp32 elements
@@ -167,6 +169,12 @@ struct GatedArgs : GemmArgs {
 template <int OP_>
 struct GatedProduct : GatedArgs {
     static constexpr int OP = OP_;
+};
+// A slice of the reduction of one tile of it.
+template <int OP_>
+struct GatedSlice : GatedProduct<OP_> {
+    static constexpr bool SPLIT = true;
+    float* partial;  // of this slice of the tile, [BM][BN]
 };
 
 }  // namespace axo

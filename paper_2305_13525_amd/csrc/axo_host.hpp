@@ -138,6 +138,7 @@ int launch_products(const axo::GemmArgs* products, int n, int la, int lb, hipStr
 enum class Tiles { small, wide, tall, mid, big };
 Tiles quickest_tiles(int Mo, int No, int R);
 double tiles_time(Tiles tiles, int Mo, int No, int R);  // estimate in us, operands in the caches
+double pair_time(int Mo, int No, int R, int la, int lb);  // two such products in one call
 axo::TileSched plan_columns(int Mo, int No, int R);
 // Whether a product fetches rows by whole cache lines on those tiles: on none (0), on whole 256-row ones (1), on all (2).
 int takes_lines_on(const axo::GemmArgs& g, int la, int lb, Tiles tiles, const axo::TileSched& sc);

@@ -35,6 +35,41 @@ struct GatedSlimCfg {
     static_assert(BM % 16 == 0 && BC % 32 == 0 && LDS_BYTES <= 160 * 1024 && (ST - 1) * LOADS < 64, "LDS of one CU, loads that a wait can count");
 };
 
+// From the sums of four columns of a row to the outputs.  x1, x2: the biases, or G and U.
+template <int OP, int PARTS>
+__device__ __forceinline__ void gated_finish(const GatedArgs& g, const f32x4 (&sum)[PARTS], const f32x4 x1, const f32x4 x2, int row, int col, int valid) {
+    auto store = [&](bf16_t* to, int64_t ld, f32x4 v) __attribute__((always_inline)) {
+        GemmArgs h;
+        h.C = to;
+        h.ldc = ld;
+        store_bf16_quad(h, v, row, col, valid);
+    };
+    if constexpr (OP == GATED_DX || OP == GATED_DW) store(g.C, g.ldc, sum[0]);
+    else
+        with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
+            constexpr int GATE = decltype(gate)::value;
+            f32x4 v, w;
+            if constexpr (OP == GATED_FWD) {
+                const f32x4 gs = sum[0] + x1, us = sum[PARTS - 1] + x2;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = gate_value<GATE>(gs[e]) * us[e];
+                store(g.C, g.ldc, v);
+                if (!g.G) return;
+                store(g.G, g.ldz, gs);
+                store(g.U, g.ldz, us);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 a = gate_both<GATE>(x1[e]);
+                    v[e] = sum[0][e] * x2[e] * a.y;
+                    w[e] = sum[0][e] * a.x;
+                }
+                store(g.C, g.ldc, v);
+                store(g.U, g.ldc, w);
+            }
+        });
+}
+
 template <int OP, int BM, int BC, int NW, int ST>
 __global__ void __launch_bounds__(NW * 64) gated_slim_kernel(GatedProduct<OP> g, GatedSlimSched sc) {
     using C = GatedSlimCfg<OP, BM, BC, NW, ST>;
@@ -228,45 +263,101 @@ __global__ void __launch_bounds__(NW * 64) gated_slim_kernel(GatedProduct<OP> g,
             }
         if (tid == 0) __hip_atomic_store(sc.counters + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    auto store = [&](bf16_t* to, int64_t ld, f32x4 v, int row, int col) __attribute__((always_inline)) {
-        GemmArgs h;
-        h.C = to;
-        h.ldc = ld;
-        store_bf16_quad(h, v, row, col, min(4, g.No - col));
-    };
-    auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < ROUNDS; ++i) {
-            const int row = i0 + quad_row(i), col = j0 + quad_col(i);
-            if (quad_row(i) < BM && row < g.Mo && col < g.No) f(i, row, col);
+    for (int i = 0; i < ROUNDS; ++i) {
+        const int row = i0 + quad_row(i), col = j0 + quad_col(i);
+        if (quad_row(i) < BM && row < g.Mo && col < g.No) gated_finish<OP>(g, sum[i], x1[i], x2[i], row, col, min(4, g.No - col));
+    }
+}
+
+// ---- 128 x 128 tiles whose reductions are cut into slices ----------------------------------------
+// For outputs of too few tiles for the CUs and reductions too long for one of them.  What a workgroup computes is a product like any other, on its slice of the operands (of both
+// products of dX), and leaves its fp32 sums in the workspace; the tiles of a slice follow each other, so that an XCD's L2 has what they share.  A second launch adds the slices
+// in ascending order and has the epilogue: a tile's last workgroup, doing that alone, would read a megabyte or more at a CU's share of the memory (128 x 13952 x 272 through the derivative
+// 32 us that way).
+struct GatedSplitSched {
+    int tiles_m, tiles_n;
+    int slices, chunks;  // of a tile's reduction, steps of 64 in each but the last
+    float* partial;      // [tile][slice][128][128]
+};
+constexpr int SPLIT_TILE = 128 * 128;
+// Where a tile's outputs are, and with two weight gradients whose.
+template <int OP>
+__device__ __forceinline__ void split_tile(const GatedSplitSched& sc, int tile, GatedArgs& g, int& i0, int& j0) {
+    int tn = tile / sc.tiles_m;
+    if (OP == GATED_DW && tn >= sc.tiles_n / 2) {
+        tn -= sc.tiles_n / 2;
+        g.B = g.B2;
+        g.C = g.U;
+    }
+    i0 = tile % sc.tiles_m * 128;
+    j0 = tn * gated_cols<OP>(128);
+}
+template <int OP, bool LINES>
+__global__ void __launch_bounds__(TILE_THREADS, 1) gated_split_kernel(GatedProduct<OP> product, GatedSplitSched sc) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    constexpr int LA = OP == GATED_DW ? MC : KC, LB = OP == GATED_FWD || OP == GATED_DW ? MC : KC;
+    const int id = xcd_run(blockIdx.x, gridDim.x), tiles = sc.tiles_m * sc.tiles_n, tile = id % tiles, slice = id / tiles;
+    GatedSlice<OP> g;
+    static_cast<GatedProduct<OP>&>(g) = product;
+    int i0, j0;
+    split_tile<OP>(sc, tile, g, i0, j0);
+    g.partial = sc.partial + ((int64_t)tile * sc.slices + slice) * SPLIT_TILE;
+    const int64_t from = (int64_t)slice * sc.chunks * TILE_BK, a = LA == KC ? from : from * g.lda, b = LB == KC ? from : from * g.ldb;
+    g.R = min(sc.chunks * TILE_BK, g.R - (int)from);
+    g.A += a;
+    g.B += b;
+    if constexpr (OP == GATED_DX) g.A2 += a;
+    if constexpr (OP == GATED_DX || OP == GATED_FWD) g.B2 += b;
+    gemm_ring_body<128, 128, 4, 2, 4, LA, LB, LINES>(g, i0, j0, smem, threadIdx.x);
+}
+// Four consecutive columns of a row of the outputs to a thread.
+constexpr int SPLIT_JOIN_THREADS = 256;
+template <int OP>
+__global__ void __launch_bounds__(SPLIT_JOIN_THREADS) gated_split_join_kernel(GatedProduct<OP> product, GatedSplitSched sc) {
+    constexpr int COLS = gated_cols<OP>(128), QPR = COLS / 4, PARTS = OP == GATED_FWD ? 2 : 1, BLOCKS = 128 * QPR / SPLIT_JOIN_THREADS;  // of a tile
+    const int tile = blockIdx.x / BLOCKS, quad = blockIdx.x % BLOCKS * SPLIT_JOIN_THREADS + threadIdx.x, r = quad / QPR, c = quad % QPR * 4;
+    GatedArgs g = product;
+    int i0, j0;
+    split_tile<OP>(sc, tile, g, i0, j0);
+    const int row = i0 + r, col = j0 + c, valid = min(4, g.No - col);
+    if (row >= g.Mo || valid <= 0) return;
+    const float* const from = sc.partial + (int64_t)tile * sc.slices * SPLIT_TILE + r * 128 + c;
+    f32x4 sum[PARTS], x1 = {0.f, 0.f, 0.f, 0.f}, x2 = x1;
+    if constexpr (OP == GATED_FWD) {
+        if (g.bias) x1 = load_bf16x4(g.bias + col, valid);
+        if (g.bias2) x2 = load_bf16x4(g.bias2 + col, valid);
+    }
+    if constexpr (OP == GATED_DACT) {
+        x1 = load_bf16x4(g.aux + (int64_t)row * g.ldaux + col, valid);
+        x2 = load_bf16x4(g.aux2 + (int64_t)row * g.ldaux + col, valid);
+    }
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) sum[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < sc.slices; s0 += 4) {  // four slices requested at a time
+        f32x4 v[4][PARTS];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q)
+                v[s][q] = s0 + s < sc.slices ? *reinterpret_cast<const f32x4*>(from + (int64_t)(s0 + s) * SPLIT_TILE + q * COLS) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) sum[q] += v[s][q];
+    }
+    if constexpr (OP == GATED_DW) {
+        if (g.epilogue == EPI_ACC_F32) {
+            float* const out = reinterpret_cast<float*>(g.C) + (int64_t)row * g.ldc + col;
+            if (valid == 4) *reinterpret_cast<f32x4*>(out) += sum[0];
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < valid) out[e] += sum[0][e];
+            return;
         }
-    };
-    if constexpr (OP == GATED_DX) each([&](int i, int row, int col) __attribute__((always_inline)) { store(g.C, g.ldc, sum[i][0], row, col); });
-    else
-        with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
-            constexpr int GATE = decltype(gate)::value;
-            each([&](int i, int row, int col) __attribute__((always_inline)) {
-                f32x4 v, w;
-                if constexpr (OP == GATED_FWD) {
-                    const f32x4 gs = sum[i][0] + x1[i], us = sum[i][PARTS - 1] + x2[i];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = gate_value<GATE>(gs[e]) * us[e];
-                    store(g.C, g.ldc, v, row, col);
-                    if (!g.G) return;
-                    store(g.G, g.ldz, gs, row, col);
-                    store(g.U, g.ldz, us, row, col);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 a = gate_both<GATE>(x1[i][e]);
-                        v[e] = sum[i][0][e] * x2[i][e] * a.y;
-                        w[e] = sum[i][0][e] * a.x;
-                    }
-                    store(g.C, g.ldc, v, row, col);
-                    store(g.U, g.ldc, w, row, col);
-                }
-            });
-        });
+    }
+    gated_finish<OP>(g, sum, x1, x2, row, col, valid);
 }
 
 }  // namespace axo

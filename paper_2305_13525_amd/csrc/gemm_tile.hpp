@@ -1594,7 +1594,16 @@ __device__ __forceinline__ void gemm_ring_body(const Args& g, const int i0, cons
     if (KT >= 2) step(IC<D - 2>{}, IC<2>{});
     step(IC<D - 1>{}, IC<1>{});
     const bool whole = i0 + BM <= g.Mo && j0 + BN <= g.No;
-    if constexpr (Args::OP == GATED_FWD) return gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
+    if constexpr (Args::SPLIT) {  // a slice's sums, rows of the tile behind each other; G's columns ahead of U's
+#pragma unroll
+        for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+            for (int b = 0; b < C::TN; ++b) {
+                const int col = TWO_B ? b / (C::TN / 2) * (BN / 2) + wn * (C::WTN / 2) + b % (C::TN / 2) * 16 : wn * C::WTN + b * 16;
+                *reinterpret_cast<f32x4*>(g.partial + (wm * C::WTM + a * 16 + (lane & 15)) * BN + col + 4 * (lane >> 4)) = acc[a][b];
+            }
+        return;
+    } else if constexpr (Args::OP == GATED_FWD) return gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
     else if constexpr (Args::OP == GATED_DACT) return gated_dact_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, whole);
     else {
     if constexpr (!SMALL || EPILOGUE == MIXED)
