@@ -106,7 +106,8 @@ size_t axo_norm_workspace_bytes(const axo_problem_t *p);
  * ws: axo_gated_workspace_bytes(p) bytes of device memory, 16-byte aligned (may be NULL when that is 0).  It begins with arrival counters that must be
  * ZERO when the call starts executing and are zero again when it has finished: zero-fill the workspace once after allocating it and leave it to calls of the
  * gated entry points, which must not overlap in time on one workspace.
- * Errors: those of axo_shard_dims; BAD_EPILOGUE (gate); NULL_PTR (also G without U), BAD_LD, MISALIGNED; BAD_ARG (shared bytes); WORKSPACE; HIP; NO_MEMORY. */
+ * Errors: those of axo_shard_dims; BAD_EPILOGUE (gate); NULL_PTR (also G without U), BAD_LD, MISALIGNED; BAD_ARG (shared bytes); WORKSPACE; BAD_SIZE (over 8388480
+ * rows in the general kernel, which takes empty reductions and operands whose spans pass 4 GiB); HIP; NO_MEMORY. */
 int axo_gated_fwd(const axo_problem_t *p, const void *X, int64_t ldx, const void *Wg, const void *Wu, int64_t ldw, const void *bg,
                   const void *bu, int gate, void *G, void *U, int64_t ldz, void *H, int64_t ldh, void *ws, size_t ws_bytes,
                   void *hip_stream);

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
 // The forward's tiles hold as many columns of Wg as of Wu, so a tile of BN columns of the two is one of BN / 2 columns of H, and the operands are read and the
 // matrix units fed as for one product of twice the columns.  dX is one product of twice the reduction.
 // Bound by the matrix units at large sizes, by the epilogue's memory where the reduction is short.  Measured, 256 x 256 tiles: forward 4096 x 8192 x 16384 with
-// G and U kept 1.53 to 1.55 ms, 1430 TFLOP/s (axo_fc_fwd on the same columns 1485); the gradient through the activation 4096 x 8192 x 16384 826 to 844 us, 1300 (axo_fc_dgrad
+// G and U kept 1.51 to 1.55 ms, 1440 TFLOP/s (axo_fc_fwd on the same columns 1485); the gradient through the activation 4096 x 8192 x 16384 826 to 844 us, 1300 (axo_fc_dgrad
 // 735 us: the rest is G and U read and a second output, which no reduction hides, since all tiles of a round come to their ends together); dX of 4096 x 7168 x 14336
 // 1.29 ms, 1310.  1001 x 1027 x 515 forward 10.1 us, through the activation 9.0.
 template <int OP>

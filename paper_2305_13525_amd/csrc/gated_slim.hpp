@@ -8,8 +8,8 @@
 // Slices: a workgroup writes its fp32 sums to the workspace and counts itself in on its tile's counter; whoever comes last adds the slices in
 // ascending order and finishes the tile, and sets the counter back to zero.  Which workgroup that is depends on timing, what it computes does not.
 // All of that goes past the L2 of an XCD by device-scope accesses, without fences (as bias_grad_split_kernel).
-// Measured, weights from memory: forward 1 x 8192 x 16384 99 us, 5.4 TB/s (a large copy 4.8, a stream of reads alone 5.8); dX of 96 x 2048 x 6144 20 us, 2.5 TB/s, its weights read once
-// from memory and by three tiles from the caches.  On the tiles of gemm_tile.hpp these take 104 and 34.
+// Measured, weights from memory: forward 1 x 8192 x 16384 99 to 101 us, 5.3 TB/s (a large copy 4.8, a stream of reads alone 5.8; on the tiles of gemm_tile.hpp 104); dX of
+// 96 x 2048 x 6144 20 us (on those tiles 34), its weights read once from memory and by three tiles from the caches, which is why slices of 128 x 128 tiles, below, take it in 17.
 #pragma once
 #include "gate.hpp"
 #include "gemm_slim.hpp"
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(NW * 64) gated_slim_kernel(GatedProduct<OP> g,
 // For outputs of too few tiles for the CUs and reductions too long for one of them.  What a workgroup computes is a product like any other, on its slice of the operands (of both
 // products of dX), and leaves its fp32 sums in the workspace; the tiles of a slice follow each other, so that an XCD's L2 has what they share.  A second launch adds the slices
 // in ascending order and has the epilogue: a tile's last workgroup, doing that alone, would read a megabyte or more at a CU's share of the memory (128 x 13952 x 272 through the derivative
-// 32 us that way).
+// 32 us that way, 15 this).  Measured: forward 1760 x 15131 x 128 28 us (on whole tiles 77), dX of 96 x 2048 x 6144 14 us and 3 for the second launch.
 struct GatedSplitSched {
     int tiles_m, tiles_n;
     int slices, chunks;  // of a tile's reduction, steps of 64 in each but the last
