@@ -400,9 +400,10 @@ GatedCut gated_cut(int Mo, int No, int R, double* us) {
     return best;
 }
 // 128 x 128 tiles in the slices that are estimated to be quickest, all on the CUs at once, and the time of that: two launches, a slice's steps or the operands' way
-// from memory, and the sums' way through the workspace.  Taken where that is a fifth less than on whole tiles, or less than what gated_cut finds.  Of 160 drawn
+// from memory, and the sums' way through the workspace.  Taken where that is less than what gated_cut finds and than on whole tiles, to 64 steps by a
+// fifth (without that margin beyond: 16 of 70 shapes 3 to 69 % quicker, none slower; with it gone below, 15 to 25 % slower at two slices).  Of 160 drawn
 // products with a split, with and without it (us): forward 1760 x 15131 x 128 28 and 77, 128 x 11305 x 1778 25 and 54, through the derivative 512 x 10200 x 512 19 and 27, dX with the weight gradients
-// 128 x 2200 x 9344 51 and 80, 5784 x 640 x 752 42 and 115, 4413 x 3952 x 184 62 and 105; slower at worst by a quarter, where two slices of fewer than 20 steps looked better.
+// 128 x 2200 x 9344 51 and 80, 5784 x 640 x 752 42 and 115, 4413 x 3952 x 184 62 and 105.
 template <int OP>
 GatedCut gated_split_cut(int Mo, int No, int R, double* us) {
     GatedCut cut;
@@ -462,7 +463,7 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     GatedCut cut;
     if (Mo <= 2048) cut = gated_cut<OP>(Mo, No, R, &us);  // never quicker beyond
     const GatedCut split = gated_split_cut<OP>(Mo, No, R, &split_us);
-    if (split_us < std::min(us, 0.8 * tiles_us)) plan.cut = split;
+    if (split_us < std::min(us, (steps_in(R) < 64 ? 0.8 : 1.0) * tiles_us)) plan.cut = split;
     else if (us < tiles_us) plan.cut = cut;
     return plan;
 }
