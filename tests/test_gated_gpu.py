@@ -387,7 +387,7 @@ def test_spans_past_4_gib():
     bu.within(dX.result(), both @ ww.T, bu.BF16 * np.abs(both @ ww.T) + bu.product_bound(both, ww.T))
 
 
-@pytest.mark.parametrize("m,k,f", [(1, 2048, 512), (24, 520, 200), (300, 256, 640)])
+@pytest.mark.parametrize("m,k,f", [(1, 2048, 512), (24, 520, 200), (300, 256, 640), (4701, 64, 120), (408, 2880, 8), (112, 704, 4720)])
 def test_same_bits_on_any_stream_and_in_graphs(m, k, f):
     d, b = inputs(m, k, f, 25), back_inputs(m, f, k, 26)
     first = forward(d, 0) + dgrad_act(b, 0)
@@ -427,7 +427,7 @@ def test_same_bits_on_any_stream_and_in_graphs(m, k, f):
 
 def test_calls_share_a_workspace():
     """Calls of several shapes, cut into different numbers of slices, one behind the other on one workspace: each gets what it gets on its own."""
-    shapes = [(1, 4096, 192), (2, 5120, 1336), (1, 9, 961), (40, 2104, 64), (1, 4095, 1566), (1, 2048, 8), (272, 10, 962)]
+    shapes = [(1, 4096, 192), (2, 5120, 1336), (1, 9, 961), (40, 2104, 64), (1, 4095, 1566), (1, 2048, 8), (272, 10, 962), (408, 2880, 8), (112, 704, 4720)]
     shared = [axo.axo_gated_tiles(bu.problem(m, k, f), op)[1][2] > 1 for m, k, f in shapes for op in (0, 2)]
     assert sum(shared) >= 6
     cases, need = [], 0
