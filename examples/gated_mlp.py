@@ -45,6 +45,7 @@ class GatedMLP:
         self.n, self.h, self.g, self.u, self.o = bf(tokens, width), bf(tokens, inner), bf(tokens, inner), bf(tokens, inner), bf(tokens, width)
         self.dg, self.du, self.dn, self.dx = bf(tokens, inner), bf(tokens, inner), bf(tokens, width), bf(tokens, width)
         self.stats = torch.empty((tokens, 2), device=DEV)
+        self._forwarded = 0  # tokens whose activations the buffers hold for a backward pass
         self._kept = {}  # workspaces of the token counts met so far
 
     def _plan(self, tokens):
@@ -55,9 +56,18 @@ class GatedMLP:
             self._kept[tokens] = up, down, [(torch.zeros(max(n, 16), dtype=torch.uint8, device=DEV), n) for n in sizes]
         return self._kept[tokens]
 
+    def _check(self, what: str, t: torch.Tensor) -> None:
+        """The calls are given addresses: what they read and write has to be there."""
+        if t.dtype != torch.bfloat16 or t.dim() != 2 or t.shape[1] != self.width or t.stride(1) != 1 or t.device != self.n.device:
+            raise ValueError(f"{what}: rows of {self.width} bfloat16 values on {self.n.device}")
+        if t.shape[0] > self.tokens:
+            raise ValueError(f"{what}: {t.shape[0]} tokens, and buffers for {self.tokens}")
+
     def forward(self, x: torch.Tensor, training: bool = True) -> torch.Tensor:
+        self._check("x", x)
         m, w, st = x.shape[0], self.w, torch.cuda.current_stream().cuda_stream
         up, down, (_, (ws, nws), _) = self._plan(m)
+        self._forwarded = m if training else 0  # n and h are overwritten either way
         save = (self.g.data_ptr(), self.u.data_ptr(), _ld(self.g)) if training else (None, None, 0)
         axo.axo_norm_fwd(up, x.data_ptr(), _ld(x), None, 0, axo.AXO_TYPE_BF16, w["gamma"].data_ptr(), w["beta"].data_ptr(), EPS, None, 0,
                          self.n.data_ptr(), _ld(self.n), self.stats.data_ptr() if training else None, st)
@@ -68,7 +78,11 @@ class GatedMLP:
         return x + self.o[:m]
 
     def backward(self, x: torch.Tensor, dy: torch.Tensor) -> torch.Tensor:
-        """Adds the weights' gradients to self.grad and returns x's."""
+        """Adds the weights' gradients to self.grad and returns x's.  x: of the last forward pass, which was one of training."""
+        self._check("x", x)
+        self._check("dy", dy)
+        if dy.shape != x.shape or x.shape[0] != self._forwarded:
+            raise ValueError(f"x has {x.shape[0]} tokens, dy {dy.shape[0]}, and the last forward pass in training had {self._forwarded}")
         w, grad, st = self.w, self.grad, torch.cuda.current_stream().cuda_stream
         up, down, ((wn, nn), (wu, nu), (wd, nd)) = self._plan(x.shape[0])
         axo.axo_fc_wgrad_acc(down, self.h.data_ptr(), _ld(self.h), dy.data_ptr(), _ld(dy), grad["wd"].data_ptr(), _ld(grad["wd"]), None, 0, st)
@@ -80,7 +94,7 @@ class GatedMLP:
                                 grad["wu"].data_ptr(), _ld(grad["wg"]), wu.data_ptr(), nu, st)
         axo.axo_norm_bwd(up, self.dn.data_ptr(), _ld(self.dn), x.data_ptr(), _ld(x), dy.data_ptr(), _ld(dy), axo.AXO_TYPE_BF16, w["gamma"].data_ptr(),
                          self.stats.data_ptr(), self.dx.data_ptr(), _ld(self.dx), grad["gamma"].data_ptr(), grad["beta"].data_ptr(), 1, wn.data_ptr(), nn, st)
-        return self.dx
+        return self.dx[:x.shape[0]]
 
     def update(self, rate: float, most: float = 1.0) -> None:
         """A step along the gradient, which is shortened to a 2-norm of `most` where it is longer."""

@@ -50,3 +50,18 @@ def test_gradients_of_the_sublayer(tokens):
     assert off(back(dx), want_dx) <= 0.01
     for k, v in want.items():
         assert off(back(net.grad[k]), v) <= 0.01, k
+
+
+def test_fewer_tokens_than_there_are_buffers_for():
+    """The same bits as from a sublayer of that size, and gradients of as many rows as there are tokens."""
+    rng = np.random.default_rng(6)
+    x, dy = bu.vec(bu.draw(rng, 40, 96)), bu.vec(bu.draw(rng, 40, 96))
+    got = []
+    for tokens in (300, 40):
+        net = gated_mlp.GatedMLP(tokens, 96, 160, seed=4)
+        got.append((net.forward(x), net.backward(x, dy).clone(), net.grad))
+    (y, dx, grad), (y2, dx2, grad2) = got
+    assert dx.shape == x.shape and torch.equal(y, y2) and torch.equal(dx, dx2)
+    assert all(torch.equal(grad[k], grad2[k]) for k in grad)
+    with pytest.raises(ValueError):
+        gated_mlp.GatedMLP(39, 96, 160).forward(x)
