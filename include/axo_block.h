@@ -107,7 +107,8 @@ size_t axo_norm_workspace_bytes(const axo_problem_t *p);
  * ZERO when the call starts executing and are zero again when it has finished: zero-fill the workspace once after allocating it and leave it to calls of the
  * gated entry points, which must not overlap in time on one workspace.
  * Errors: those of axo_shard_dims; BAD_EPILOGUE (gate); NULL_PTR (also G without U), BAD_LD, MISALIGNED; BAD_ARG (shared bytes); WORKSPACE; BAD_SIZE (over 8388480
- * rows in the general kernel, which takes empty reductions and operands whose spans pass 4 GiB); HIP; NO_MEMORY. */
+ * rows in the general kernel, which takes empty reductions, operands whose spans pass 4 GiB and outputs of more 256 x 128 tiles than a launch takes, 8388607,
+ * the columns of both projections counted); HIP; NO_MEMORY. */
 int axo_gated_fwd(const axo_problem_t *p, const void *X, int64_t ldx, const void *Wg, const void *Wu, int64_t ldw, const void *bg,
                   const void *bu, int gate, void *G, void *U, int64_t ldz, void *H, int64_t ldh, void *ws, size_t ws_bytes,
                   void *hip_stream);

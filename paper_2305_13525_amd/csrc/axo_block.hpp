@@ -439,11 +439,11 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     if (Mo == 0 || No == 0) return plan;
     // as one product: twice the columns, or twice the reduction
     const int64_t cols = OP == axo::GATED_FWD ? 2 * (int64_t)No : No, red = OP == axo::GATED_DX ? 2 * (int64_t)R : R;
-    if (R == 0 || cols > INT32_MAX || red > INT32_MAX || !grid_fits(tiles_in(Mo, 64) * tiles_in((int)cols, 64), axo::TILE_THREADS)) {
+    if (R == 0 || cols > INT32_MAX || red > INT32_MAX || !grid_fits(tiles_in(Mo, 256) * tiles_in((int)cols, 128), axo::TILE_THREADS)) {
         plan.general = true;
         return plan;
     }
-    plan.tiles = quickest_tiles(Mo, (int)cols, (int)red);
+    plan.tiles = quickest_tiles(Mo, (int)cols, (int)red);  // 64 x 64 ones where those fit a launch as well, the other small ones for a round of CUs alone
     const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);
     const double tiles_us = std::max(tiles_time(plan.tiles, Mo, (int)cols, (int)red) * GATED_TILES[OP][(int)plan.tiles], 3.0 + weights / 5.0);
     const int64_t small_tiles = tiles_in(Mo, 64) * tiles_in((int)cols, 64);

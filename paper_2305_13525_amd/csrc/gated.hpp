@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(GATED_MAP_THREADS) gated_map_kernel(GatedMapAr
 }
 
 // The block's products for any sizes and spans, 64-bit indices, 128 x 128 tiles staged through registers as gemm_generic_kernel: what is left to it are
-// empty reductions and operands whose spans pass 4 GiB.  Forward 4096 x 8192 x 16384 12.7 ms, an eighth of the tiles' rate.
+// empty reductions, operands whose spans pass 4 GiB and outputs of a billion rows or columns, whose 256-row tiles are too many for a launch.  Forward
+// 4096 x 8192 x 16384 12.7 ms, an eighth of the tiles' rate.
 template <int OP>
 __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
     constexpr int LB = OP == GATED_FWD ? MC : KC, SUMS = OP == GATED_FWD ? 2 : 1;

@@ -288,3 +288,18 @@ def test_quick_calls(name):
         for m in range(len(base)):
             assert outcome(quick, *base[:m]) == outcome(wrapper, *base[:m])
     assert n > 100
+
+
+# tokens x width x inner width whose outputs have more 64 x 64 tiles than a launch takes, but not more 256-row ones: the large tiles, as axo_fc_fwd
+@pytest.mark.parametrize("T,K,N", [(4200000, 64, 4096), (8388608, 64, 2048), (33554432, 64, 512)])
+def test_tall_outputs_run_on_tiles(T, K, N):
+    assert axo.axo_gated_tiles(P(T, K, N), axo.AXO_GATED_OP_FWD)[1] == (256, 128, 1)
+    assert axo.axo_gated_tiles(P(T, 2 * N, K), axo.AXO_GATED_OP_DGRAD_ACT)[1] == (256, 256, 1)
+    assert axo.axo_gated_tiles(P(T, 2 * N, K), axo.AXO_GATED_OP_DGRAD)[1] == (256, 256, 1)
+
+
+def test_what_no_launch_takes_goes_to_the_general_kernel():
+    """A billion rows of one column: no tiles, and more rows than the general kernel has a grid for."""
+    p = P(2 ** 31 - 1, 8, 8)
+    assert axo.axo_gated_tiles(p, axo.AXO_GATED_OP_FWD)[1] == (0, 0, 0)
+    assert call("axo_gated_fwd", p=p, **{k: 8 for k in ("ldx", "ldw", "ldz", "ldh")}) == BAD_SIZE

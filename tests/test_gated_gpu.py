@@ -452,3 +452,23 @@ def test_calls_share_a_workspace():
         for c, want in zip(cases[::-1] if turn % 2 else cases, alone[::-1] if turn % 2 else alone):
             got = run(*c, ws, need)
             assert all(np.array_equal(a.result(), b.result()) for a, b in zip(got, want)), (turn, c[2])
+
+
+def test_more_rows_than_small_tiles_of_a_launch():
+    """4.2 million rows, whose 64 x 64 tiles are more than a launch takes.  The rows repeat every 1024, which is whole tiles, so the results do, bit for bit."""
+    m, k, f, period = 4200000, 64, 4096, 1024
+    d, p = inputs(period, k, f, 41), bu.problem(m, k, f)
+    assert axo.axo_gated_tiles(p, axo.AXO_GATED_OP_FWD)[1] == (256, 128, 1)
+    X = bu.vec(d["x"]).repeat(m // period + 1, 1)[:m]
+    Wg, Wu = bu.Mat(d["wg"]), bu.Mat(d["wu"])
+    H = torch.full((m, f), float("nan"), dtype=torch.bfloat16, device=bu.DEV)
+    ws, n = workspace(p)
+    axo.axo_gated_fwd(p, X.data_ptr(), k, Wg.ptr, Wu.ptr, Wg.ld, None, None, 0, None, None, 0, H.data_ptr(), f, ws.data_ptr(), n, bu.stream())
+    h, g, u = ob.gated_fwd(d["x"], d["wg"], d["wu"], 0)
+    bu.within(H[:period].double().cpu().numpy(), h, bu.gated_fwd_bounds(d["x"], d["wg"], d["wu"], g, u, ob.gate(g, 0)[0])[0])
+    first = H[:period].view(torch.int16)
+    for at in range(0, m, 256 * period):
+        some = H[at:at + 256 * period].view(torch.int16)
+        whole = some.shape[0] // period * period
+        assert torch.equal(some[:whole].view(-1, period, f), first.expand(whole // period, period, f)), at
+        assert torch.equal(some[whole:], first[:some.shape[0] - whole]), at
