@@ -472,3 +472,33 @@ def test_more_rows_than_small_tiles_of_a_launch():
         whole = some.shape[0] // period * period
         assert torch.equal(some[:whole].view(-1, period, f), first.expand(whole // period, period, f)), at
         assert torch.equal(some[whole:], first[:some.shape[0] - whole]), at
+
+
+@pytest.mark.parametrize("m,k,f", [(300, 100, 200), (129, 33, 130)])
+def test_spans_past_4_gib_over_several_workgroups(m, k, f):
+    """Every matrix in rows 16 MB apart: the general kernel on outputs of several ragged tiles, reductions of several turns, G and U kept, biases."""
+    gap = (1 << 23) + 8
+    check_forward(inputs(m, k, f, 42), 0, True, (True, True), gap)
+    check_forward(inputs(m, k, f, 43), 2, False, (False, True), gap)
+    check_dgrad_act(back_inputs(m, f, k, 44), 1, gap)
+    check_products(m, k, f, 45, gap)
+
+
+def test_weight_gradients_of_spans_past_4_gib():
+    """Sizes whose tiles are cut into slices, with operands that the slices' 32-bit offsets do not reach: X, dG and dU, or X alone."""
+    m, k, f = 4701, 64, 120
+    p = bu.problem(m, k, f)
+    assert axo.axo_gated_tiles(p, axo.AXO_GATED_OP_WGRAD)[1][2] > 1
+    rng = np.random.default_rng(46)
+    d = [bu.draw(rng, m, c) for c in (k, f, f)]
+    for gaps in ((1 << 19, 1 << 19), (1 << 19, 0), (0, 1 << 19)):
+        X, dG, dU = (bu.Mat(a, g) for a, g in zip(d, (gaps[0], gaps[1], gaps[1])))
+        dWg, dWu = bu.Out(k, f), bu.Out(k, f)
+        acc = [bu.Mat(np.full((k, f), 0.5), 0, wide=True) for _ in range(2)]
+        ws, n = workspace(p)
+        axo.axo_gated_wgrad(p, X.ptr, X.ld, dG.ptr, dU.ptr, dG.ld, dWg.ptr, dWu.ptr, dWg.ld, ws.data_ptr(), n, bu.stream())
+        axo.axo_gated_wgrad_acc(p, X.ptr, X.ld, dG.ptr, dU.ptr, dG.ld, acc[0].ptr, acc[1].ptr, acc[0].ld, ws.data_ptr(), n, bu.stream())
+        for out, a, z in ((dWg, acc[0], d[1]), (dWu, acc[1], d[2])):
+            want, err = d[0].T @ z, bu.product_bound(d[0].T, z)
+            bu.within(out.result(), want, bu.BF16 * np.abs(want) + err)
+            bu.within(a.numpy(), want + 0.5, err + 2 * bu.FP32 * np.abs(want + 0.5))
