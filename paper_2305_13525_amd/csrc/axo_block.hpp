@@ -8,6 +8,7 @@
 #include "axo_host.hpp"
 #include "gated.hpp"
 #include "gated_slim.hpp"
+#include "last_used.hpp"
 #include "norm.hpp"
 
 static_assert((int)AXO_GATED_OP_FWD == axo::GATED_FWD && (int)AXO_GATED_OP_DGRAD_ACT == axo::GATED_DACT && (int)AXO_GATED_OP_DGRAD == axo::GATED_DX && (int)AXO_GATED_OP_WGRAD == axo::GATED_DW, "one numbering");
@@ -479,27 +480,23 @@ GatedPlan gated_wgrad_plan(int K, int N, int M) {
 }
 
 // The plans of the calls that a problem is passed to, as the block's projections and as the layer behind it, and the largest workspace among them.  A
-// plan takes a microsecond; a thread keeps those of the problems that it called last.
+// plan takes up to a microsecond; a thread keeps those of the last sixteen sizes that it called with.
 struct GatedPlans {
-    int64_t M = -1, K = -1, N = -1;
     GatedPlan of[4];
     size_t bytes = 0;
 };
 const GatedPlans& gated_plans(const Shard& s) {
-    static thread_local GatedPlans kept[16];
-    GatedPlans& p = kept[(size_t)(s.M + 31 * s.Kl + 1009 * s.Nl) % 16];
-    if (p.M == s.M && p.K == s.Kl && p.N == s.Nl) return p;
-    const int M = (int)s.M, K = (int)s.Kl, N = (int)s.Nl;
-    p.of[axo::GATED_FWD] = gated_plan<axo::GATED_FWD>(M, N, K);
-    p.of[axo::GATED_DACT] = gated_plan<axo::GATED_DACT>(M, K, N);
-    p.of[axo::GATED_DX] = gated_plan<axo::GATED_DX>(M, K, N);
-    p.of[axo::GATED_DW] = gated_wgrad_plan(K, N, M);
-    p.bytes = 0;
-    for (const GatedPlan& plan : p.of) p.bytes = std::max(p.bytes, plan.cut.bytes);
-    p.M = s.M;
-    p.K = s.Kl;
-    p.N = s.Nl;
-    return p;
+    static thread_local axo::LastUsed<GatedPlans, 16> kept;
+    return kept.get(s.M, s.Kl, s.Nl, [&] {
+        const int M = (int)s.M, K = (int)s.Kl, N = (int)s.Nl;
+        GatedPlans p;
+        p.of[axo::GATED_FWD] = gated_plan<axo::GATED_FWD>(M, N, K);
+        p.of[axo::GATED_DACT] = gated_plan<axo::GATED_DACT>(M, K, N);
+        p.of[axo::GATED_DX] = gated_plan<axo::GATED_DX>(M, K, N);
+        p.of[axo::GATED_DW] = gated_wgrad_plan(K, N, M);
+        for (const GatedPlan& plan : p.of) p.bytes = std::max(p.bytes, plan.cut.bytes);
+        return p;
+    });
 }
 
 template <int OP, int KIND>
