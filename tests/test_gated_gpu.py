@@ -502,3 +502,22 @@ def test_weight_gradients_of_spans_past_4_gib():
             want, err = d[0].T @ z, bu.product_bound(d[0].T, z)
             bu.within(out.result(), want, bu.BF16 * np.abs(want) + err)
             bu.within(a.numpy(), want + 0.5, err + 2 * bu.FP32 * np.abs(want + 0.5))
+
+
+def test_hundreds_of_millions_of_columns():
+    """600 million columns through the activation, on 9.4 million 64 x 64 tiles.  They repeat every 1024, and so do the results."""
+    m, period, n = 3, 1024, 8
+    f = period * 585938
+    d, p = back_inputs(m, period, n, 47), bu.problem(m, f, n)
+    assert axo.axo_gated_tiles(p, axo.AXO_GATED_OP_DGRAD_ACT)[1] == (64, 64, 1)
+    dY, W = bu.vec(d["dy"]), bu.vec(d["w"]).repeat(f // period, 1)
+    G, U = (bu.vec(d[c]).repeat(1, f // period) for c in "gu")
+    dG, dU = (torch.full((m, f), float("nan"), dtype=torch.bfloat16, device=bu.DEV) for _ in range(2))
+    ws, size = workspace(p)
+    axo.axo_gated_dgrad_act(p, dY.data_ptr(), n, W.data_ptr(), n, G.data_ptr(), U.data_ptr(), f, 1, dG.data_ptr(), dU.data_ptr(), f, ws.data_ptr(), size, bu.stream())
+    dh, (value, slope) = d["dy"] @ d["w"].T, ob.gate(d["g"], 1)
+    bounds = bu.gated_dact_bounds(bu.product_bound(d["dy"], d["w"].T), dh, d["g"], d["u"], value, slope)
+    for t, want, bound in zip((dG, dU), ob.gated_dact(dh, d["g"], d["u"], 1), bounds):
+        bu.within(t[:, :period].double().cpu().numpy(), want, bound)
+        bits = t.view(torch.int16).view(m, f // period, period)
+        assert torch.equal(bits, bits[:, :1].expand(-1, f // period, -1))
