@@ -24,7 +24,8 @@
  *     axo_norm_bwd_part gives two sums per row, which the caller adds up over the K axis, and axo_norm_bwd_apply finishes.
  *   - the activation of the gated block belongs behind the sum over the K axis.  Where that has size 1, axo_gated_fwd and (for the layer
  *     behind the block, whose data gradient is summed over its N axis) axo_gated_dgrad_act are whole; elsewhere two axo_fc_fwd, the
- *     all-reduce and axo_gated_act give H, and axo_fc_dgrad, the all-reduce and axo_gated_dact give (dG, dU).
+ *     all-reduce and axo_gated_act give H, and axo_fc_dgrad, the all-reduce and axo_gated_dact give (dG, dU).  Neither call refuses
+ *     the other grids: axo_gated_fwd then gives this shard's parts of G and U, and an H of those parts, which is no part of the layer's.
  */
 #ifndef AXO_BLOCK_H
 #define AXO_BLOCK_H

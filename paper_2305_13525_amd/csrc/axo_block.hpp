@@ -126,7 +126,8 @@ int launch_norm_bwd_groups(axo::NormBwdArgs& g, hipStream_t st) {
     return launch_norm_join(g, st);
 }
 // A workgroup has 512 threads, and of bf16 rows 1024 where there are more rows than workgroups of 512 take at once: the same bytes under way.  2^25 values, 512 and 1024
-// threads (us): 64 columns bf16 67, 57, fp32 87, 90; 512 columns 65, 54 and 86, 89; 2048 columns 64, 53 and 86, 90.  (1000 x 64 bf16: 6.9, 8.0.)
+// threads (us): 64 columns bf16 67, 57, fp32 87, 90; 512 columns 65, 54 and 86, 89; 2048 columns 64, 53 and 86, 90.  (1000 x 64 bf16: 6.9, 8.0.)  Those sizes are bound by
+// bandwidth; fp32 rows that take two turns of 512 threads and one of 1024, some thousand of 1027, were not compared.
 template <typename T, int LANES, int CH>
 int launch_norm_bwd_rows(axo::NormBwdArgs& g, hipStream_t st) {
     constexpr int GROUPS = 512 / LANES;

@@ -5,7 +5,9 @@
 // All of it moves each element once or twice and computes some ten operations on it: bound by memory.  Rows are therefore kept in registers between
 // their statistics and their outputs, and as many lanes share a row as leave each of them whole 16-byte loads.
 // Measured, bf16 with a residual: forward 4096 x 12288 75.8 us (5.3 TB/s; a large copy reaches 4.8), one row of 4096 3.1 us; backward 8192 x 7168 97.7 us with
-// dgamma and dbeta (4.8 TB/s), 1001 x 1027 in fp32 9.9 us, two launches of 6.9 and 2.7 to 3.7.
+// dgamma and dbeta (4.8 TB/s), 1001 x 1027 in fp32 9.9 us, two launches of 6.9 and 2.7 to 3.7.  In halves, a shard of 8192 x 3584 of two: statistics with a residual 35 us
+// bf16 and 61 fp32 (5.0 and 5.7 TB/s), the other half 33 and 43 (3.6, 4.1); backward 31 and 48 (3.8, 3.6: a second launch), 46 and 75 (5.2, 5.5).  4096 x 1536 of
+// eight: 8.3 and 16.7, 17.7 and 19.2 (every lane reads the row's eight pairs, twice, ahead of its output; of 2048 columns 11.5 with two and 13.7 with four), 11.6 and 14.2, 12.1 and 20.0.
 #pragma once
 #include <type_traits>
 
