@@ -1,0 +1,381 @@
+"""What ends a sublayer and updates its weights, as timed cases: a product with the residual in its epilogue, the norms either side of a residual
+addition with its gate, and the orthogonalised update of a weight, on buffers that the program owns.
+
+A case gives tokens T, widths K and N, and which operator is called:
+
+  how = "ortho"         O = Newton-Schulz iterate of the gradient G[K x N] over its Frobenius norm, STEPS times
+                        X <- a X + b (X X^T) X + c (X X^T)^2 X
+  how = "resnorm_fwd"   S = X + SCALE * gate * norm_a(B), Y = norm_b(S), with the rows' statistics kept for the backward pass
+  how = "resnorm_bwd"   from dY and the residual stream's gradient dS: dX, dB and the gradients of both norms' vectors and of the gate
+  how = "add_fwd"       Y = R + SCALE * act(X W + b); with `save` also the pre-activation, which the backward pass reads
+  how = "add_bwd"       dZ = SCALE * dY * act'(Z)
+
+  act   0 none, 1 a bias alone, 2 bias and GELU (tanh form), 3 bias and GELU (erf form)
+  na    norm behind the block: 0 none, 1 layer norm, 2 root mean square
+  nb    norm ahead of the next one: 1, 2
+  wide  the residual stream (X, S, dS, dX of the norms; R, Y, dY of the product) or the gradient G in fp32, else bf16
+  gap   elements between the end of a matrix row (rounded up to 8) and the next row
+
+Inputs: activations N(0, 1), weights and biases N(0, 0.02), gammas around 1, gates around 0.5; a gradient's rows and columns have scales of
+their own, as those of a layer's features do.  bf16 unless said otherwise, accumulators fp32.
+"""
+import functools
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+SIGMA_W = 0.02
+EPS = 1e-5
+ORTHO_EPS = 1e-7
+SCALE = 0.5
+STEPS = 5
+A, B, C = 3.4445, -4.7750, 2.0315
+
+
+def _case(name, how, T=0, K=0, N=0, act=0, na=0, nb=0, wide=False, save=False, gap=0):
+    return {"name": name, "how": how, "T": T, "K": K, "N": N, "act": act, "na": na, "nb": nb, "wide": wide, "save": save, "gap": gap}
+
+
+def listed():
+    return [
+        # a narrow projection of a small model: seventeen dependent steps with next to nothing to do in each
+        _case("ortho_small", "ortho", K=128, N=512),
+        # a tall weight of which nothing is a multiple of anything, its fp32 master gradient with padded rows
+        _case("ortho_odd", "ortho", K=1001, N=515, wide=True, gap=8),
+        # a 2048-wide model's projection to queries, keys and values
+        _case("ortho_2048", "ortho", K=2048, N=6144),
+        # the weight from a 16384-wide inner layer back to a 4096-wide stream: the largest
+        _case("ortho_16384", "ortho", K=16384, N=4096),
+        # one token of an answer between two sublayers
+        _case("resnorm_fwd_token", "resnorm_fwd", T=1, K=4096, na=2, nb=2),
+        # the tokens of one of four token shards of a 12288-wide model
+        _case("resnorm_fwd_12288", "resnorm_fwd", T=4096, K=12288, na=1, nb=1),
+        # ragged rows of an fp32 stream
+        _case("resnorm_bwd_odd", "resnorm_bwd", T=1001, K=1027, na=2, nb=1, wide=True, gap=8),
+        # a 7168-wide model's block in training
+        _case("resnorm_bwd_7168", "resnorm_bwd", T=8192, K=7168, na=1, nb=1),
+        # one token through the second half of an MLP: the weights are what is read
+        _case("add_fwd_token", "add_fwd", T=1, K=16384, N=4096, act=1),
+        # a ragged prompt, what the backward pass needs is kept
+        _case("add_fwd_odd", "add_fwd", T=1001, K=1027, N=515, act=3, wide=True, save=True, gap=8),
+        # a training step's tokens through one GPU's share of an MLP's second half
+        _case("add_fwd_16384", "add_fwd", T=4096, K=16384, N=2048, act=1),
+        # back through an activation ahead of a residual addition
+        _case("add_bwd_6000", "add_bwd", T=4000, N=6000, act=2, wide=True),
+    ]
+
+
+def _log_size(rng, lo, hi):
+    """A size spread over the logarithm of [lo, hi]: a third of them any number, a third multiples of 8, the rest multiples of 128."""
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    unit = rng.choice((1, 8, 128))
+    return min(hi, max(1, lo if v < lo else int(v / unit + 0.5) * unit or unit))
+
+
+def draw(rng):
+    how = rng.choice(("ortho", "ortho", "resnorm_fwd", "resnorm_bwd", "add_fwd", "add_fwd", "add_bwd"))
+    gap = rng.choice((0, 0, 0, 8, 64))
+    while True:
+        t, k, n = _log_size(rng, 1, 16384), _log_size(rng, 32, 16384), _log_size(rng, 32, 16384)
+        if how == "ortho":
+            if 1.0 * min(k, n) ** 2 * max(k, n) <= 1e11:
+                t = 0
+                break
+        elif how == "add_fwd":
+            if 1.0 * t * k * n <= 1.4e11:
+                break
+        elif t * k <= 1 << 26:
+            n = 0
+            break
+    if how == "add_bwd":
+        k, n = 0, k
+    c = _case("", how, t, k, n, gap=gap, wide=rng.random() < 0.4)
+    del c["name"]
+    if how.startswith("resnorm"):
+        c["na"], c["nb"] = rng.randint(0, 2), rng.randint(1, 2)
+    elif how == "add_fwd":
+        c["act"] = rng.randint(0, 3)
+        c["save"] = c["act"] >= 2 and rng.random() < 0.5
+    elif how == "add_bwd":
+        c["act"] = rng.randint(1, 3)
+    return c
+
+
+def _rows(rows, cols, gap, dtype=torch.bfloat16):
+    return torch.zeros((rows, (cols + 7) // 8 * 8 + gap), dtype=dtype, device=DEV)[:, :cols]
+
+
+def _inputs(case, seed):
+    """What the operator reads, made on the GPU from the seed alone."""
+    how, m, k, n, gap = case["how"], case["T"], case["K"], case["N"], case["gap"]
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+
+    def normal(rows, cols, sigma=1.0, mean=0.0, dtype=torch.bfloat16, gap=gap):
+        a = torch.empty((rows, (cols + 7) // 8 * 8 + gap), dtype=dtype, device=DEV)
+        a.normal_(mean, sigma, generator=gen)
+        return a[:, :cols]
+
+    stream = torch.float32 if case["wide"] else torch.bfloat16
+    t = {}
+    if how == "ortho":
+        g = normal(k, n, 1e-3, dtype=torch.float32)
+        t["G"] = _rows(k, n, gap, stream)
+        t["G"].copy_(g * torch.exp(normal(k, 1, 0.5, dtype=torch.float32, gap=0)) * torch.exp(normal(1, n, 0.5, dtype=torch.float32, gap=0)))
+        return t
+    if how.startswith("resnorm"):
+        t["B"], t["X"] = normal(m, k, 1.5, 0.25), normal(m, k, 3.0, 0.5, stream)
+        for name, mean in (("gamma_a", 1.0), ("beta_a", 0.0), ("gate", 0.5), ("gamma_b", 1.0), ("beta_b", 0.0)):
+            t[name] = normal(1, k, 0.1, mean, gap=0)[0]
+        if how == "resnorm_bwd":
+            b, stats = t["B"].double(), []
+
+            def normed(v, kind):
+                mean = v.mean(1, keepdim=True) if kind == 1 else torch.zeros_like(v[:, :1])
+                rstd = torch.rsqrt((v - mean).square().mean(1, keepdim=True) + EPS) if kind else torch.ones_like(mean)
+                stats.extend((mean, rstd))
+                return (v - mean) * rstd
+
+            z = normed(b, case["na"]) * t["gamma_a"].double() + t["beta_a"].double()
+            t["S"] = _rows(m, k, gap, stream)
+            t["S"].copy_(t.pop("X").double() + SCALE * t["gate"].double() * z)  # what the forward pass left
+            normed(t["S"].double(), case["nb"])
+            t["stats"] = torch.cat(stats, 1).float()
+            t["dY"], t["dS"] = normal(m, k), normal(m, k, 1.0, 0.0, stream)
+        return t
+    if how == "add_bwd":
+        t["dY"] = normal(m, n, 1.0, 0.0, stream)
+        if case["act"] >= 2:
+            t["Z"] = normal(m, n, 1.5)
+        return t
+    t["X"], t["W"], t["R"] = normal(m, k), normal(k, n, SIGMA_W), normal(m, n, 3.0, 0.5, stream)
+    if case["act"]:
+        t["bias"] = normal(1, n, SIGMA_W, gap=0)[0]
+    return t
+
+
+def prepare(case, seed):
+    """The inputs, and the buffers that the program has for the outputs."""
+    how, m, k, n, gap = case["how"], case["T"], case["K"], case["N"], case["gap"]
+    t = _inputs(case, seed)
+    stream = torch.float32 if case["wide"] else torch.bfloat16
+    if how == "ortho":
+        t["O"] = _rows(k, n, gap)
+    elif how == "resnorm_fwd":
+        t["S"], t["Y"], t["stats"] = _rows(m, k, gap, stream), _rows(m, k, gap), torch.zeros((m, 4), device=DEV)
+    elif how == "resnorm_bwd":
+        t["dX"], t["dB"] = _rows(m, k, gap, stream), _rows(m, k, gap)
+        for name in ("dgamma_a", "dbeta_a", "dgate", "dgamma_b", "dbeta_b"):
+            t[name] = torch.zeros(k, device=DEV)
+    elif how == "add_fwd":
+        t["Y"] = _rows(m, n, gap, stream)
+        if case["save"]:
+            t["Z"] = _rows(m, n, gap)
+    else:
+        t["dZ"] = _rows(m, n, gap)
+    t["case"], t["stream"] = case, torch.cuda.current_stream().cuda_stream
+    return t
+
+
+def _act(z, act):
+    if act < 2:
+        return z
+    if act == 2:
+        return 0.5 * z * (1.0 + torch.tanh(math.sqrt(2.0 / math.pi) * (z + 0.044715 * z * z * z)))
+    return 0.5 * z * (1.0 + torch.erf(z * math.sqrt(0.5)))
+
+
+def _dact(z, act):
+    if act == 2:
+        th = torch.tanh(math.sqrt(2.0 / math.pi) * (z + 0.044715 * z * z * z))
+        return 0.5 * (1.0 + th) + 0.5 * z * (1.0 - th * th) * math.sqrt(2.0 / math.pi) * (1.0 + 3.0 * 0.044715 * z * z)
+    return 0.5 * (1.0 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) * math.sqrt(0.5 / math.pi)
+
+
+def _norm(v, kind):
+    """(normed rows, mean, 1 / deviation)"""
+    mean = v.mean(1, keepdim=True) if kind == 1 else torch.zeros_like(v[:, :1])
+    d = v - mean
+    rstd = torch.rsqrt((d * d).mean(1, keepdim=True) + EPS) if kind else torch.ones_like(mean)
+    return d * rstd, mean, rstd
+
+
+def _norm_back(g, h, rstd, kind):
+    """The gradient of a norm's input from that of its normed rows h."""
+    if kind == 0:
+        return g
+    d = g - h * (g * h).mean(1, keepdim=True)
+    return rstd * (d - g.mean(1, keepdim=True) if kind == 1 else d)
+
+
+def _plain(t):
+    case, how = t["case"], t["case"]["how"]
+    stream = torch.float32 if case["wide"] else torch.bfloat16
+    if how == "ortho":
+        x = t["G"].float()
+        tall = x.shape[0] > x.shape[1]
+        if tall:
+            x = x.t()
+        x = x / (torch.sqrt((x * x).sum()) + ORTHO_EPS)
+        for _ in range(STEPS):
+            gram = x @ x.t()
+            x = A * x + (B * gram + C * (gram @ gram)) @ x
+        return {"O": (x.t() if tall else x).to(torch.bfloat16)}
+    if how == "resnorm_fwd":
+        h, mean_a, rstd_a = _norm(t["B"].float(), case["na"])
+        s = (t["X"].float() + SCALE * t["gate"].float() * (h * t["gamma_a"].float() + t["beta_a"].float())).to(stream)
+        y, mean_b, rstd_b = _norm(s.float(), case["nb"])  # of the stream as it is stored
+        return {"S": s, "Y": (y * t["gamma_b"].float() + t["beta_b"].float()).to(torch.bfloat16), "stats": torch.cat((mean_a, rstd_a, mean_b, rstd_b), 1)}
+    if how == "resnorm_bwd":
+        mean_a, rstd_a, mean_b, rstd_b = t["stats"].split(1, 1)
+        ha, hb, dy = (t["B"].float() - mean_a) * rstd_a, (t["S"].float() - mean_b) * rstd_b, t["dY"].float()
+        ds = t["dS"].float() + _norm_back(dy * t["gamma_b"].float(), hb, rstd_b, case["nb"])
+        gate, gamma, beta = t["gate"].float(), t["gamma_a"].float(), t["beta_a"].float()
+        dz = SCALE * gate * ds
+        return {"dX": ds.to(stream), "dB": _norm_back(dz * gamma, ha, rstd_a, case["na"]).to(torch.bfloat16),
+                "dgamma_a": (dz * ha).sum(0), "dbeta_a": dz.sum(0), "dgate": (SCALE * ds * (ha * gamma + beta)).sum(0),
+                "dgamma_b": (dy * hb).sum(0), "dbeta_b": dy.sum(0)}
+    if how == "add_bwd":
+        dz = SCALE * t["dY"].float()
+        return {"dZ": (dz * _dact(t["Z"].float(), case["act"]) if case["act"] >= 2 else dz).to(torch.bfloat16)}
+    z = t["X"].float() @ t["W"].float()
+    if case["act"]:
+        z = z + t["bias"].float()
+    out = {"Y": (t["R"].float() + SCALE * _act(z, case["act"])).to(stream)}
+    if case["save"]:
+        out["Z"] = z.to(torch.bfloat16)
+    return out
+
+
+@functools.lru_cache(maxsize=64)
+def _plan(how, T, K, N):
+    """The problem statement of a layer and the workspace that the operator wants, kept as a program keeps them."""
+    import paper_2305_13525_amd as axo
+
+    p = axo.Problem.make((1, 1, 1), (0, 0, 0), T, K, N)
+    if how == "add_bwd":
+        return axo, p, None, 0
+    size = {"ortho": axo.axo_ortho_workspace_bytes, "add_fwd": axo.axo_fc_add_workspace_bytes}.get(how, axo.axo_resnorm_workspace_bytes)(p)
+    return axo, p, torch.zeros(max(size, 16), dtype=torch.uint8, device=DEV).data_ptr(), size
+
+
+def _called(t):
+    case, how, stream = t["case"], t["case"]["how"], t["stream"]
+    axo, p, ws, ws_bytes = _plan("resnorm" if how.startswith("resnorm") else how, case["T"], case["K"], case["N"])
+    kind = axo.AXO_TYPE_F32 if case["wide"] else axo.AXO_TYPE_BF16
+    if how == "ortho":
+        G, O = t["G"], t["O"]
+        axo.axo_ortho(p, G.data_ptr(), G.stride(0), kind, STEPS, None, ORTHO_EPS, O.data_ptr(), O.stride(0), ws, ws_bytes, stream)
+        return {"O": O}
+    if how == "resnorm_fwd":
+        Bm, X, S, Y = t["B"], t["X"], t["S"], t["Y"]
+        axo.axo_resnorm_fwd(p, Bm.data_ptr(), Bm.stride(0), X.data_ptr(), X.stride(0), kind, case["na"], t["gamma_a"].data_ptr(), t["beta_a"].data_ptr(),
+                            t["gate"].data_ptr(), SCALE, case["nb"], t["gamma_b"].data_ptr(), t["beta_b"].data_ptr(), EPS, S.data_ptr(), S.stride(0),
+                            Y.data_ptr(), Y.stride(0), t["stats"].data_ptr(), stream)
+        return {"S": S, "Y": Y, "stats": t["stats"]}
+    if how == "resnorm_bwd":
+        dY, dS, Bm, S, dX, dB = t["dY"], t["dS"], t["B"], t["S"], t["dX"], t["dB"]
+        axo.axo_resnorm_bwd(p, dY.data_ptr(), dY.stride(0), dS.data_ptr(), dS.stride(0), Bm.data_ptr(), Bm.stride(0), S.data_ptr(), S.stride(0), kind,
+                            case["na"], t["gamma_a"].data_ptr(), t["beta_a"].data_ptr(), t["gate"].data_ptr(), SCALE, case["nb"], t["gamma_b"].data_ptr(),
+                            t["stats"].data_ptr(), dX.data_ptr(), dX.stride(0), dB.data_ptr(), dB.stride(0), t["dgamma_a"].data_ptr(),
+                            t["dbeta_a"].data_ptr(), t["dgate"].data_ptr(), t["dgamma_b"].data_ptr(), t["dbeta_b"].data_ptr(), 0, ws, ws_bytes, stream)
+        return {name: t[name] for name in ("dX", "dB", "dgamma_a", "dbeta_a", "dgate", "dgamma_b", "dbeta_b")}
+    if how == "add_bwd":
+        dY, Z, dZ = t["dY"], t.get("Z"), t["dZ"]
+        axo.axo_fc_add_dact(p, dY.data_ptr(), dY.stride(0), kind, None if Z is None else Z.data_ptr(), 0 if Z is None else Z.stride(0), case["act"], SCALE,
+                            dZ.data_ptr(), dZ.stride(0), stream)
+        return {"dZ": dZ}
+    X, W, R, Y, Z, bias = t["X"], t["W"], t["R"], t["Y"], t.get("Z"), t.get("bias")
+    axo.axo_fc_add(p, X.data_ptr(), X.stride(0), W.data_ptr(), W.stride(0), None if bias is None else bias.data_ptr(), case["act"], R.data_ptr(), R.stride(0),
+                   kind, SCALE, None if Z is None else Z.data_ptr(), 0 if Z is None else Z.stride(0), Y.data_ptr(), Y.stride(0), ws, ws_bytes, stream)
+    return {"Y": Y, "Z": Z} if case["save"] else {"Y": Y}
+
+
+def run(state):
+    return _called(state) if own else _plain(state)
+
+
+def work(case):
+    """Each input read once, each output written once; of a symmetric product one half."""
+    how, m, k, n = case["how"], case["T"], case["K"], case["N"]
+    e = 4.0 if case["wide"] else 2.0
+    if how == "ortho":
+        s, l = min(k, n), max(k, n)
+        return {"bytes": (e + 2.0) * k * n, "flops": STEPS * (s * (s + 1.0) * l + s * s * (s + 1.0) + 2.0 * s * s * l)}
+    if how == "resnorm_fwd":
+        return {"bytes": m * k * (2.0 + e + e + 2.0) + 10.0 * k + 16.0 * m, "flops": 18.0 * m * k}
+    if how == "resnorm_bwd":
+        return {"bytes": m * k * (2.0 + e + 2.0 + e + e + 2.0) + 28.0 * k + 16.0 * m, "flops": 32.0 * m * k}
+    if how == "add_bwd":
+        return {"bytes": m * n * (e + 2.0 + (2.0 if case["act"] >= 2 else 0.0)), "flops": 12.0 * m * n}
+    return {"bytes": 2.0 * (m * k + k * n) + m * n * (2 * e + (2.0 if case["save"] else 0.0)) + 2.0 * n, "flops": 2.0 * m * k * n + 10.0 * m * n}
+
+
+def exact(case, seed):
+    t = {name: v.double() for name, v in _inputs(case, seed).items()}
+    how, m, act = case["how"], case["T"], case["act"]
+
+    def gelu(z):
+        """(value, derivative) from the derivative of z P(z): P + z P'."""
+        if act == 2:
+            inner = math.sqrt(8.0 / math.pi) * (z + 0.044715 * z ** 3)
+            prob = torch.sigmoid(inner)
+            slope = prob * torch.sigmoid(-inner) * math.sqrt(8.0 / math.pi) * (1.0 + 0.134145 * z ** 2)
+        elif act == 3:
+            prob = 0.5 * torch.erfc(-z / math.sqrt(2.0))
+            slope = torch.exp(-z ** 2 / 2.0) / math.sqrt(2.0 * math.pi)
+        else:
+            return z, torch.ones_like(z)
+        return z * prob, prob + z * slope
+
+    if how == "ortho":
+        # the odd polynomial as a product with a matrix function on the narrower side, by Horner's rule: X (a + M (b + c M)), M = X^T X
+        flip = t["G"].shape[1] > t["G"].shape[0]
+        x = t["G"].t() if flip else t["G"]
+        x = x / (torch.linalg.vector_norm(x) + ORTHO_EPS)
+        one = torch.eye(x.shape[1], dtype=torch.float64, device=DEV)
+        for _ in range(STEPS):
+            mat = torch.mm(x.t(), x)
+            x = torch.mm(x, torch.addmm(A * one, mat, B * one + C * mat))
+        return {"O": x.t() if flip else x}
+    if how == "add_bwd":
+        return {"dZ": SCALE * t["dY"] * (gelu(t["Z"])[1] if act >= 2 else 1.0)}
+    if how == "add_fwd":
+        z = torch.mm(t["X"], t["W"]) + (t["bias"] if act else 0.0)
+        got = {"Y": t["R"] + SCALE * gelu(z)[0]}
+        if case["save"]:
+            got["Z"] = z
+        return got
+
+    def moments(v, kind):
+        var, mean = torch.var_mean(v, dim=1, correction=0)
+        if kind == 1:
+            return mean, (var + EPS) ** -0.5
+        return torch.zeros_like(mean), (var + mean ** 2 + EPS) ** -0.5 if kind == 2 else torch.ones_like(mean)
+
+    if how == "resnorm_fwd":
+        ma, ra = moments(t["B"], case["na"])
+        s = t["X"] + SCALE * t["gate"] * (t["gamma_a"] * ((t["B"] - ma.view(m, 1)) * ra.view(m, 1)) + t["beta_a"])
+        held = s.to(torch.float32 if case["wide"] else torch.bfloat16).double()
+        mb, rb = moments(held, case["nb"])
+        return {"S": s, "Y": (held - mb.view(m, 1)) * rb.view(m, 1) * t["gamma_b"] + t["beta_b"], "stats": torch.stack((ma, ra, mb, rb), 1)}
+
+    def through(g, h, rstd, kind):
+        """J^T g of h = (v - mean(v)) / deviation, by its projections on h and on ones."""
+        if kind == 0:
+            return g
+        out = g - h * ((g * h).sum(1) / g.shape[1]).view(m, 1)
+        if kind == 1:
+            out = out - (g.sum(1) / g.shape[1]).view(m, 1)
+        return out * rstd.view(m, 1)
+
+    ma, ra, mb, rb = t["stats"].unbind(1)
+    ha, hb = (t["B"] - ma.view(m, 1)) * ra.view(m, 1), (t["S"] - mb.view(m, 1)) * rb.view(m, 1)
+    ds = through(t["dY"] * t["gamma_b"], hb, rb, case["nb"]) + t["dS"]
+    sums, sums_h = ds.sum(0), (ds * ha).sum(0)
+    return {"dX": ds, "dB": through(SCALE * ds * t["gate"] * t["gamma_a"], ha, ra, case["na"]),
+            "dgamma_a": SCALE * t["gate"] * sums_h, "dbeta_a": SCALE * t["gate"] * sums, "dgate": SCALE * (t["gamma_a"] * sums_h + t["beta_a"] * sums),
+            "dgamma_b": (t["dY"] * hb).sum(0), "dbeta_b": t["dY"].sum(0)}
