@@ -256,15 +256,16 @@ def _plan(how, T, K, N):
     import paper_2305_13525_amd as axo
 
     p = axo.Problem.make((1, 1, 1), (0, 0, 0), T, K, N)
-    if how == "add_bwd":
-        return axo, p, None, 0
-    size = {"ortho": axo.axo_ortho_workspace_bytes, "add_fwd": axo.axo_fc_add_workspace_bytes}.get(how, axo.axo_resnorm_workspace_bytes)(p)
-    return axo, p, torch.zeros(max(size, 16), dtype=torch.uint8, device=DEV).data_ptr(), size
+    size = 0
+    if how != "add_bwd":
+        size = getattr(axo, {"ortho": "axo_ortho_workspace_bytes", "add_fwd": "axo_fc_add_workspace_bytes"}.get(how, "axo_resnorm_workspace_bytes"))(p)
+    return axo, p, torch.zeros(max(size, 16), dtype=torch.uint8, device=DEV), size
 
 
 def _called(t):
     case, how, stream = t["case"], t["case"]["how"], t["stream"]
-    axo, p, ws, ws_bytes = _plan("resnorm" if how.startswith("resnorm") else how, case["T"], case["K"], case["N"])
+    axo, p, buffer, ws_bytes = _plan("resnorm" if how.startswith("resnorm") else how, case["T"], case["K"], case["N"])
+    ws = buffer.data_ptr()
     kind = axo.AXO_TYPE_F32 if case["wide"] else axo.AXO_TYPE_BF16
     if how == "ortho":
         G, O = t["G"], t["O"]
