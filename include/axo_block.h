@@ -4,7 +4,8 @@
  *
  *   n = norm(x + r)                        axo_norm_fwd
  *   h = act(n Wg + bg) * (n Wu + bu)       axo_gated_fwd        (a layer of two weight matrices, K -> N each)
- *   y = h Wd                               axo_fc_fwd           (the layer behind it, N -> K)
+ *   y = h Wd                               axo_fc_fwd           (the layer behind it, N -> K; with its residual: axo_fc_add, and the norms around the addition:
+ *                                                               axo_resnorm_fwd, both of axo_residual.h)
  *
  * and back: axo_gated_dgrad_act takes dY through Wd and the product to (dG, dU), axo_gated_dgrad and axo_gated_wgrad give the
  * gradients of n, Wg and Wu, axo_norm_bwd those of x, gamma and beta; axo_fc_wgrad gives dWd, axo_bias_grad the biases'.

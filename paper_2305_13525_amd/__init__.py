@@ -21,3 +21,8 @@ from .block import (  # noqa: F401
     axo_gated_wgrad_acc, axo_gated_workspace_bytes, axo_norm_apply, axo_norm_bwd,
     axo_norm_bwd_apply, axo_norm_bwd_part, axo_norm_fwd, axo_norm_part, axo_norm_workspace_bytes,
 )
+from .residual import (  # noqa: F401
+    AXO_NORM_LAYER, AXO_NORM_NONE, AXO_NORM_RMS, axo_fc_add, axo_fc_add_dact, axo_fc_add_workspace_bytes, axo_resnorm_bwd, axo_resnorm_fwd,
+    axo_resnorm_workspace_bytes,
+)
+from .update import AXO_ORTHO_MOST_STEPS, axo_ortho, axo_ortho_workspace_bytes  # noqa: F401

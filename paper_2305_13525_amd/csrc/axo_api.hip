@@ -1549,3 +1549,5 @@ int axo_layer_step_tiles(const axo_layer_ext_t* layers, int n_layers, int* tiles
 }  // extern "C"
 
 #include "axo_block.hpp"  // the entry points of include/axo_block.h
+#include "axo_residual.hpp"  // of include/axo_residual.h
+#include "axo_ortho.hpp"  // of include/axo_update.h

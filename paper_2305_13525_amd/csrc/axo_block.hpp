@@ -26,7 +26,7 @@ inline unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)std::ma
 
 // A call's matrices: what it reads and what it writes.  An output that shares a byte with an input or another output is refused.
 struct Buffers {
-    Range in[6], out[4];
+    Range in[10], out[8];  // of resnorm_bwd, which has most: 9 and 8
     int n_in = 0, n_out = 0;
     void reads(const void* p, int64_t ld, int64_t rows, int64_t cols, int elem) {
         if (matrix_range(p, ld, rows, cols, elem, &in[n_in])) ++n_in;
@@ -270,7 +270,7 @@ template <int OP>
 bool gated_spans_ok(const GatedArgs& g) {
     auto fits = [](int64_t elems) { return elems * 2 < (int64_t)0xFFFF0000; };
     const int64_t walked = ((int64_t)g.R + 2 * axo::TILE_BK - 1) / (2 * axo::TILE_BK) * (2 * axo::TILE_BK);
-    return fits(256 * g.lda + walked) && fits(OP == axo::GATED_FWD ? walked * g.ldb + 256 : 256 * g.ldb + walked);
+    return fits(256 * g.lda + walked) && fits(axo::GATED_LB<OP> == axo::MC ? walked * g.ldb + 256 : 256 * g.ldb + walked);
 }
 
 // Rows of the outputs that straddle cache lines are stored plainly (store_row), but past the caches where the forward pass writes more than they keep for
@@ -278,7 +278,7 @@ bool gated_spans_ok(const GatedArgs& g) {
 // G and U kept, straddled 2048 x 2048 x 6008 87 and 95, 4096 x 2048 x 8200 271 and 241.
 template <int OP>
 bool gated_plain(const GatedArgs& g) {
-    const bool straddles = ((reinterpret_cast<uintptr_t>(g.C) | (uintptr_t)(g.ldc * 2)) & 127) != 0;
+    const bool straddles = ((reinterpret_cast<uintptr_t>(g.C) | (uintptr_t)(g.ldc * (OP == axo::FC_ADD && g.wide ? 4 : 2))) & 127) != 0;
     return straddles && (OP != axo::GATED_FWD || (int64_t)g.Mo * g.No * (g.G ? 6 : 2) <= (int64_t)128 << 20);
 }
 
@@ -300,7 +300,7 @@ int launch_gated_on(const GatedArgs& g, Tiles tiles, const axo::TileSched& sc, h
         if (tiles == Tiles::mid) return launch_gated_tiles<axo::MidCfg, OP>(axo::gated_mid_kernel<OP, PLAIN, ALL>, &raised[2], g, 128, 128, st);
     }
     // Forward ring tiles fetch one operand by lines at most and half-width ones none (takes_lines), so there is no forward of kind 2 on 256-row tiles.
-    constexpr int MIXED = OP == axo::GATED_FWD && LINES == 2 ? 1 : LINES;
+    constexpr int MIXED = axo::GATED_LB<OP> == axo::MC && LINES == 2 ? 1 : LINES;
     constexpr int lds = LINES != 0 ? axo::LINES_LDS_BYTES : axo::MIX_LDS_BYTES;
     auto kern = axo::gated_mixed_kernel<OP, PLAIN, MIXED>;
     if (!raise_lds_limit(reinterpret_cast<const void*>(kern), lds, &raised[3])) return AXO_ERR_HIP;
@@ -319,7 +319,7 @@ int launch_gated_tiles_of(const GatedArgs& g, Tiles tiles, int cols, int red, hi
         switch (takes_lines_on(as_one, axo::KC, axo::GATED_LB<OP>, tiles, sc)) {
             case 2: return launch_gated_on<OP, true, 2>(g, tiles, sc, st);
             case 1:
-                if constexpr (OP == axo::GATED_FWD)
+                if constexpr (axo::GATED_LB<OP> == axo::MC)
                     if (!gated_plain<OP>(g)) return launch_gated_on<OP, false, 1>(g, tiles, sc, st);
                 return launch_gated_on<OP, true, 1>(g, tiles, sc, st);
             default: break;
@@ -343,11 +343,14 @@ struct GatedSlim {
     int rows, cols, waves, stages;  // `cols`: of the output
     double fixed, rate, alone, latency, tbs, join, each;
 };
-constexpr GatedSlim GATED_SLIM[3][4] = {
+constexpr GatedSlim GATED_SLIM[5][4] = {
     {{16, 32, 4, 3, 3.26, 39.4, 67.2, 2.37, 3.78, 2.31, 1.21}, {32, 32, 4, 3, 2.85, 42.6, 64.6, 2.99, 3.14, 3.92, 1.53},
      {16, 64, 2, 4, 3.10, 51.8, 97.2, 2.65, 4.87, 3.79, 2.04}, {16, 128, 2, 2, 4.73, 49.3, 50.0, 3.14, 6.18, 4.74, 0.30}},
     {{16, 32, 4, 3, 4.32, 87.9, 126.6, 0.88, 6.72, 1.20, 0.66}, {32, 32, 4, 3, 3.01, 73.9, 155.4, 1.44, 5.48, 2.59, 1.84}, {}, {}},
-    {{16, 32, 4, 3, 4.16, 71.8, 78.6, 1.04, 5.69, 0.71, 0.28}, {32, 32, 4, 3, 3.16, 87.1, 115.1, 1.50, 4.63, 2.34, 1.24}, {}, {}}};
+    {{16, 32, 4, 3, 4.16, 71.8, 78.6, 1.04, 5.69, 0.71, 0.28}, {32, 32, 4, 3, 3.16, 87.1, 115.1, 1.50, 4.63, 2.34, 1.24}, {}, {}},
+    {},
+    {{16, 32, 4, 3, 3.26, 39.4, 67.2, 2.37, 3.78, 2.31, 1.21}, {32, 32, 4, 3, 2.85, 42.6, 64.6, 2.99, 3.14, 3.92, 1.53},
+     {16, 64, 2, 4, 3.10, 51.8, 97.2, 2.65, 4.87, 3.79, 2.04}, {16, 128, 2, 2, 4.73, 49.3, 50.0, 3.14, 6.18, 4.74, 0.30}}};
 // Rows of 256 bytes of either weight (the fourth kind) are for tokens of one tile that read more than the caches hold: there they are the quickest, 1.2 times quicker than 64 x 128
 // tiles (1 x 8192 x 16384 97 us, with rows of 128 bytes 109, on those tiles 104; where rows lie a multiple of 4 KiB apart, a column of 128 bytes
 // lies in half of each of its DRAM pages).  With less to read they are not.
@@ -355,7 +358,7 @@ constexpr double GATED_WIDE_MB = 200.0;
 // The same for the tiles of gemm_tile.hpp: what their estimates have to be multiplied with for these products (small, wide, tall, mid, big; medians of the same
 // shapes), which read weights from memory and have longer epilogues.  Whatever is estimated quicker is taken: over those shapes the choice is 1.29 (forward), 1.63 and 1.99 times
 // quicker than these tiles throughout, 3 to 5 % slower than the best of all, and by more than 5 % slower than these tiles for two or three shapes in a hundred.
-constexpr double GATED_TILES[3][5] = {{1.06, 1.66, 1.66, 1.21, 1.03}, {0.93, 1.37, 1.37, 1.41, 1.55}, {0.88, 1.47, 1.47, 1.21, 1.08}};
+constexpr double GATED_TILES[5][5] = {{1.06, 1.66, 1.66, 1.21, 1.03}, {0.93, 1.37, 1.37, 1.41, 1.55}, {0.88, 1.47, 1.47, 1.21, 1.08}, {}, {1.0, 1.4, 1.4, 1.2, 1.05}};
 
 // How a product is cut into split-reduction tiles.
 struct GatedCut {
@@ -369,11 +372,14 @@ constexpr int GATED_SPLIT = 4;  // the kind of 128 x 128 tiles in slices
 // off, eight chunks 3 to 7 %).
 int64_t gated_slices(int64_t tiles, int64_t chunks) { return std::max<int64_t>(1, std::min<int64_t>({NUM_CU / tiles, chunks / 16, 16})); }
 
+// Weight matrices of a product.
+template <int OP>
+constexpr int gated_matrices() { return OP == axo::GATED_DACT || OP == axo::FC_ADD ? 1 : 2; }
 // The quickest cut of a product (Mo x No, reductions of R) and the estimate of it.
 template <int OP>
 GatedCut gated_cut(int Mo, int No, int R, double* us) {
     const int64_t chunks = steps_in(R) * (OP == axo::GATED_DX ? 2 : 1);
-    const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);  // MB
+    const double weights = 2e-6 * No * (double)R * gated_matrices<OP>();  // MB
     GatedCut best;
     *us = 1e30;
     for (int k = 0; k < 4; ++k) {
@@ -414,7 +420,7 @@ GatedCut gated_split_cut(int Mo, int No, int R, double* us) {
     for (int64_t asked = 2; asked <= 16 && asked * tiles <= NUM_CU; ++asked) {
         const int64_t per = (steps + asked - 1) / asked, slices = (steps + per - 1) / per;
         const double step = OP == axo::GATED_DX ? 0.9 : 0.45;
-        const double operands = 2e-6 * R * (OP == axo::GATED_DX ? 2.0 * Mo + 2.0 * No : Mo + (OP == axo::GATED_DACT ? 1.0 : 2.0) * No);  // MB
+        const double operands = 2e-6 * R * (OP == axo::GATED_DX ? 2.0 * Mo + 2.0 * No : Mo + (double)gated_matrices<OP>() * No);  // MB
         const double t = 8.5 + std::max(per * step, operands / 5.5) + 0.02 * (double)(tiles * slices);
         if (per < 4 || t >= *us) continue;
         *us = t;
@@ -446,7 +452,7 @@ GatedPlan gated_plan(int Mo, int No, int R) {
         return plan;
     }
     plan.tiles = quickest_tiles(Mo, (int)cols, (int)red);  // 64 x 64 ones where those fit a launch as well, the other small ones for a round of CUs alone
-    const double weights = 2e-6 * No * (double)R * (OP == axo::GATED_DACT ? 1 : 2);
+    const double weights = 2e-6 * No * (double)R * gated_matrices<OP>();
     const double tiles_us = std::max(tiles_time(plan.tiles, Mo, (int)cols, (int)red) * GATED_TILES[OP][(int)plan.tiles], 3.0 + weights / 5.0);
     const int64_t small_tiles = tiles_in(Mo, 64) * tiles_in((int)cols, 64);
     const bool round_of_wide = tiles_in(Mo, 64) * tiles_in((int)cols, 128) <= NUM_CU;
@@ -454,7 +460,7 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     // 64 x 64 tiles that leave some CUs two and others one: a 64 x 128 tile for each CU is quicker, from four steps of a reduction on forward and from ten through the
     // activation's derivative, where G and U of a tile wait for its end.  Of 55 such shapes where 64 x 64 tiles were taken, forward 5 to 56 % over four steps (350 x 5928 x 1453 55 us
     // and 37, 1001 x 1027 x 515 12.1 and 10.1) and 0 to -5 % at two; backward 2 to 14 % from ten steps on (700 x 4000 x 1500 26.0 and 22.9), -10 to 3 % below.
-    if (OP != axo::GATED_DX && plan.tiles == Tiles::small && round_of_wide && small_tiles > NUM_CU && steps_in(R) >= (OP == axo::GATED_FWD ? 4 : 10)) plan.tiles = Tiles::wide;
+    if (OP != axo::GATED_DX && plan.tiles == Tiles::small && round_of_wide && small_tiles > NUM_CU && steps_in(R) >= (OP == axo::GATED_DACT ? 10 : 4)) plan.tiles = Tiles::wide;
     // Short reductions through the derivative are its reads of G and U and its stores, which go on beside each other where a CU has two tiles: 64 x 64 ones,
     // while there are few of them.  Of 126 shapes with reductions of 32 to 1024: for 128 x 128 tiles, to four steps and two a CU, 42 to 51 % quicker (2638 x 32 x 640 8.6 us and 6.0);
     // for 256 x 256 ones to nine a CU and four steps 0 to 50 % (876 x 192 x 8576 28.6 and 19.1), to six and sixteen steps -1 to 28 %; beyond, 11 % quicker to 27 % slower.
@@ -483,8 +489,8 @@ GatedPlan gated_wgrad_plan(int K, int N, int M) {
 // The plans of the calls that a problem is passed to, as the block's projections and as the layer behind it, and the largest workspace among them.  A
 // plan takes up to a microsecond; a thread keeps those of the last sixteen sizes that it called with.
 struct GatedPlans {
-    GatedPlan of[4];
-    size_t bytes = 0;
+    GatedPlan of[5];
+    size_t bytes = 0;  // of the first four; the product with a residual has a workspace of its own
 };
 const GatedPlans& gated_plans(const Shard& s) {
     static thread_local axo::LastUsed<GatedPlans, 16> kept;
@@ -496,6 +502,7 @@ const GatedPlans& gated_plans(const Shard& s) {
         p.of[axo::GATED_DX] = gated_plan<axo::GATED_DX>(M, K, N);
         p.of[axo::GATED_DW] = gated_wgrad_plan(K, N, M);
         for (const GatedPlan& plan : p.of) p.bytes = std::max(p.bytes, plan.cut.bytes);
+        p.of[axo::FC_ADD] = gated_plan<axo::FC_ADD>(M, N, K);
         return p;
     });
 }
@@ -538,7 +545,7 @@ int launch_gated(const GatedArgs& g, const Shard& s, void* ws, hipStream_t st) {
     if (g.Mo == 0 || g.No == 0) return AXO_OK;
     const GatedPlan& plan = gated_plans(s).of[OP];
     if (plan.general || !gated_spans_ok<OP>(g)) return launch_gated_generic<OP>(g, st);
-    switch (plan.cut.kind) {
+    switch (plan.cut.kind) {  // of the sizes alone; kinds that an operation has not are never its plan's
         case 0: return launch_gated_slim<OP, 0>(g, plan.cut, ws, st);
         case 1: return launch_gated_slim<OP, 1>(g, plan.cut, ws, st);
         case 2: return launch_gated_slim<OP, 2>(g, plan.cut, ws, st);

@@ -15,6 +15,14 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 typedef uint16_t bf16_t;  // bf16 bit pattern in memory
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+// One 16 x 16 x 32 matrix instruction on operands that are held as bf16x8 whichever type they are of.
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 
 // Operand layouts of C[i,j] = sum_r A(i,r) * B(j,r):
 //   KC: the reduction index r is contiguous in memory   (element (i,r) at i*ld + r)
@@ -34,12 +42,15 @@ enum Epilogue {
 //   GATED_DACT  one product, taken through the derivative of that
 //   GATED_DX    the sum of two products, A B^T + A2 B2^T
 //   GATED_DW    one of two products with the same A (a tile like any other; split tiles know it)
-enum GatedOp { NOT_GATED = -1, GATED_FWD = 0, GATED_DACT = 1, GATED_DX = 2, GATED_DW = 3 };
+//   FC_ADD      one product behind such a block (or any layer): bias, activation, scale, and a residual that it is added to
+enum GatedOp { NOT_GATED = -1, GATED_FWD = 0, GATED_DACT = 1, GATED_DX = 2, GATED_DW = 3, FC_ADD = 4 };
 
 // One GEMM as the kernels see it.
 struct GemmArgs {
     static constexpr int OP = NOT_GATED;
     static constexpr bool SPLIT = false;
+    static constexpr bool F16 = false;  // operands of fp16 instead of bf16
+    static constexpr bool OWN = false;  // tiles are finished by Args::finish
     const bf16_t* A; int64_t lda;
     const bf16_t* B; int64_t ldb;
     bf16_t* C;       int64_t ldc;   // EPI_ACC_F32: C points to fp32 and ldc counts fp32 elements
@@ -163,7 +174,10 @@ struct GatedArgs : GemmArgs {
     bf16_t* G;            // outputs beside C: G and U of the forward pass or nullptr, pitch ldz
     bf16_t* U;            // ... dU of the backward pass, where C is dG (pitch ldc)
     int64_t ldz;
-    int gate;             // Gate
+    int gate;             // Gate; of FC_ADD the forward Epilogue that is applied
+    // FC_ADD: C = aux + scale act(sum + bias), C and aux (pitches ldc, ldaux in elements) of fp32 where `wide`, else bf16; aux nullptr: zeros; G the pre-activation
+    int wide;
+    float scale;
 };
 // The same, for tiles that do OP_.
 template <int OP_>

@@ -12,6 +12,7 @@
 
 #include "../../include/axo.h"
 #include "../../include/axo_block.h"
+#include "../../include/axo_residual.h"
 
 typedef union {
     const void *ptr;
@@ -32,7 +33,7 @@ typedef struct {
     PyObject *wrapper;
 } entry;
 
-#define MOST_ARGUMENTS 18
+#define MOST_ARGUMENTS 31
 
 static PyObject *problem_type, *raise_if;
 
@@ -59,7 +60,7 @@ static int call_bias_grad_ws(void *f, const value *a) {
         a[0].ptr, a[1].ptr, a[2].i64, (float *)a[3].ptr, a[4].i32, (void *)a[5].ptr, a[6].size, (void *)a[7].ptr);
 }
 
-/* Functions of axo_block.h.  (Outputs are passed as pointers to const: on this ABI the same.) */
+/* Functions of axo_block.h and axo_residual.h.  (Outputs are passed as pointers to const: on this ABI the same.) */
 static int call_norm_fwd(void *f, const value *a) {
     return ((int (*)(const axo_problem_t *, const void *, int64_t, const void *, int64_t, int, const void *, const void *, float, const void *,
         int64_t, const void *, int64_t, const void *, const void *))f)(a[0].ptr, a[1].ptr, a[2].i64, a[3].ptr, a[4].i64, a[5].i32, a[6].ptr,
@@ -118,11 +119,36 @@ static int call_gated_wgrad(void *f, const value *a) {
         void *, size_t, const void *))f)(a[0].ptr, a[1].ptr, a[2].i64, a[3].ptr, a[4].ptr, a[5].i64, a[6].ptr, a[7].ptr, a[8].i64, a[9].ptr,
         a[10].size, a[11].ptr);
 }
+static int call_fc_add(void *f, const value *a) {
+    return ((int (*)(const axo_problem_t *, const void *, int64_t, const void *, int64_t, const void *, int, const void *, int64_t, int,
+        float, const void *, int64_t, const void *, int64_t, const void *, size_t, const void *))f)(a[0].ptr, a[1].ptr, a[2].i64, a[3].ptr,
+        a[4].i64, a[5].ptr, a[6].i32, a[7].ptr, a[8].i64, a[9].i32, a[10].f32, a[11].ptr, a[12].i64, a[13].ptr, a[14].i64, a[15].ptr,
+        a[16].size, a[17].ptr);
+}
+static int call_fc_add_dact(void *f, const value *a) {
+    return ((int (*)(const axo_problem_t *, const void *, int64_t, int, const void *, int64_t, int, float, const void *, int64_t, const void
+        *))f)(a[0].ptr, a[1].ptr, a[2].i64, a[3].i32, a[4].ptr, a[5].i64, a[6].i32, a[7].f32, a[8].ptr, a[9].i64, a[10].ptr);
+}
+static int call_resnorm_fwd(void *f, const value *a) {
+    return ((int (*)(const axo_problem_t *, const void *, int64_t, const void *, int64_t, int, int, const void *, const void *, const void
+        *, float, int, const void *, const void *, float, const void *, int64_t, const void *, int64_t, const void *, const void
+        *))f)(a[0].ptr, a[1].ptr, a[2].i64, a[3].ptr, a[4].i64, a[5].i32, a[6].i32, a[7].ptr, a[8].ptr, a[9].ptr, a[10].f32, a[11].i32,
+        a[12].ptr, a[13].ptr, a[14].f32, a[15].ptr, a[16].i64, a[17].ptr, a[18].i64, a[19].ptr, a[20].ptr);
+}
+static int call_resnorm_bwd(void *f, const value *a) {
+    return ((int (*)(const axo_problem_t *, const void *, int64_t, const void *, int64_t, const void *, int64_t, const void *, int64_t, int,
+        int, const void *, const void *, const void *, float, int, const void *, const void *, const void *, int64_t, const void *, int64_t,
+        const void *, const void *, const void *, const void *, const void *, int, const void *, size_t, const void *))f)(a[0].ptr,
+        a[1].ptr, a[2].i64, a[3].ptr, a[4].i64, a[5].ptr, a[6].i64, a[7].ptr, a[8].i64, a[9].i32, a[10].i32, a[11].ptr, a[12].ptr,
+        a[13].ptr, a[14].f32, a[15].i32, a[16].ptr, a[17].ptr, a[18].ptr, a[19].i64, a[20].ptr, a[21].i64, a[22].ptr, a[23].ptr, a[24].ptr,
+        a[25].ptr, a[26].ptr, a[27].i32, a[28].ptr, a[29].size, a[30].ptr);
+}
 
 enum {
     FWD, DGRAD, WGRAD, DGRAD_ACT, WGRAD_ACC, BIAS_GRAD, BIAS_GRAD_WS, BIAS_GRAD_STATIC, ENTRIES,
     NORM_FWD = ENTRIES, NORM_PART, NORM_APPLY, NORM_BWD, NORM_BWD_PART, NORM_BWD_APPLY, GATED_FWD, GATED_ACT, GATED_DACT, GATED_DGRAD_ACT,
-    GATED_DGRAD, GATED_WGRAD, GATED_WGRAD_ACC, ALL_ENTRIES
+    GATED_DGRAD, GATED_WGRAD, GATED_WGRAD_ACC, BLOCK_ENTRIES,
+    FC_ADD = BLOCK_ENTRIES, FC_ADD_DACT, RESNORM_FWD, RESNORM_BWD, ALL_ENTRIES
 };
 static entry entries[ALL_ENTRIES] = {
     {"axo_fc_fwd", "pvlvlvivlvzv", 9, {{0}}, call_fwd, 0, 0},
@@ -146,6 +172,10 @@ static entry entries[ALL_ENTRIES] = {
     {"axo_gated_dgrad", "pvvlvvlvlvzv", 9, {{0}}, call_gated_dgrad, 0, 0},
     {"axo_gated_wgrad", "pvlvvlvvlvzv", 9, {{0}}, call_gated_wgrad, 0, 0},
     {"axo_gated_wgrad_acc", "pvlvvlvvlvzv", 9, {{0}}, call_gated_wgrad, 0, 0},
+    {"axo_fc_add", "pvlvlvivlifvlvlvzv", 15, {{0}}, call_fc_add, 0, 0},
+    {"axo_fc_add_dact", "pvlivlifvlv", 10, {{0}}, call_fc_add_dact, 0, 0},
+    {"axo_resnorm_fwd", "pvlvliivvvfivvfvlvlvv", 20, {{0}}, call_resnorm_fwd, 0, 0},
+    {"axo_resnorm_bwd", "pvlvlvlvliivvvfivvvlvlvvvvvivzv", 27, {{0}}, call_resnorm_bwd, 0, 0},
 };
 
 /* One argument other than the problem; 0 if it is not of a plain kind. */
@@ -235,8 +265,12 @@ ENTRY(GATED_DGRAD_ACT)
 ENTRY(GATED_DGRAD)
 ENTRY(GATED_WGRAD)
 ENTRY(GATED_WGRAD_ACC)
+ENTRY(FC_ADD)
+ENTRY(FC_ADD_DACT)
+ENTRY(RESNORM_FWD)
+ENTRY(RESNORM_BWD)
 
-/* set_up(Problem, {name: wrapper}, raise_if): once, when binding.py is imported; set_up_block, when block.py is. */
+/* set_up(Problem, {name: wrapper}, raise_if): once, when binding.py is imported; set_up_block and set_up_residual, when block.py and residual.py are. */
 static PyObject *set_up_some(PyObject *args, int first, int end) {
     PyObject *type, *wrappers, *raise;
     if (!PyArg_ParseTuple(args, "OO!O", &type, &PyDict_Type, &wrappers, &raise)) return NULL;
@@ -278,7 +312,11 @@ static PyObject *set_up(PyObject *self, PyObject *args) {
 }
 static PyObject *set_up_block(PyObject *self, PyObject *args) {
     (void)self;
-    return set_up_some(args, ENTRIES, ALL_ENTRIES);
+    return set_up_some(args, ENTRIES, BLOCK_ENTRIES);
+}
+static PyObject *set_up_residual(PyObject *self, PyObject *args) {
+    (void)self;
+    return set_up_some(args, BLOCK_ENTRIES, ALL_ENTRIES);
 }
 static PyObject *bind(PyObject *self, PyObject *args) {
     (void)self;
@@ -286,7 +324,11 @@ static PyObject *bind(PyObject *self, PyObject *args) {
 }
 static PyObject *bind_block(PyObject *self, PyObject *args) {
     (void)self;
-    return bind_some(args, ENTRIES, ALL_ENTRIES);
+    return bind_some(args, ENTRIES, BLOCK_ENTRIES);
+}
+static PyObject *bind_residual(PyObject *self, PyObject *args) {
+    (void)self;
+    return bind_some(args, BLOCK_ENTRIES, ALL_ENTRIES);
 }
 
 #define METHOD(ID, NAME, SIGNATURE) {NAME, (PyCFunction)(void (*)(void))py_##ID, METH_FASTCALL | METH_KEYWORDS, NAME SIGNATURE "\n--\n\n"}
@@ -312,10 +354,16 @@ static PyMethodDef methods[] = {
     METHOD(GATED_DGRAD, "axo_gated_dgrad", "($module, p, dG, dU, lddz, Wg, Wu, ldw, dX, lddx, ws=None, ws_bytes=0, stream=None, check=True)"),
     METHOD(GATED_WGRAD, "axo_gated_wgrad", "($module, p, X, ldx, dG, dU, lddz, dWg, dWu, lddw, ws=None, ws_bytes=0, stream=None, check=True)"),
     METHOD(GATED_WGRAD_ACC, "axo_gated_wgrad_acc", "($module, p, X, ldx, dG, dU, lddz, dWg, dWu, lddw, ws=None, ws_bytes=0, stream=None, check=True)"),
+    METHOD(FC_ADD, "axo_fc_add", "($module, p, X, ldx, W, ldw, bias, epilogue, R, ldr, type, scale, Z, ldz, Y, ldy, ws=None, ws_bytes=0, stream=None, check=True)"),
+    METHOD(FC_ADD_DACT, "axo_fc_add_dact", "($module, p, dY, lddy, type, Z, ldz, epilogue, scale, dZ, lddz, stream=None, check=True)"),
+    METHOD(RESNORM_FWD, "axo_resnorm_fwd", "($module, p, B, ldb, X, ldx, type, norm_a, gamma_a, beta_a, gate, scale, norm_b, gamma_b, beta_b, eps, S, lds, Y, ldy, stats, stream=None, check=True)"),
+    METHOD(RESNORM_BWD, "axo_resnorm_bwd", "($module, p, dY, lddy, dS, ldds, B, ldb, S, lds, type, norm_a, gamma_a, beta_a, gate, scale, norm_b, gamma_b, stats, dX, lddx, dB, lddb, dgamma_a, dbeta_a, dgate, dgamma_b, dbeta_b, accumulate=0, ws=None, ws_bytes=0, stream=None, check=True)"),
     {"set_up", set_up, METH_VARARGS, "set_up(Problem, wrappers, raise_if)"},
     {"bind", bind, METH_VARARGS, "bind(addresses, version)"},
     {"set_up_block", set_up_block, METH_VARARGS, "set_up_block(Problem, wrappers, raise_if)"},
     {"bind_block", bind_block, METH_VARARGS, "bind_block(addresses, version)"},
+    {"set_up_residual", set_up_residual, METH_VARARGS, "set_up_residual(Problem, wrappers, raise_if)"},
+    {"bind_residual", bind_residual, METH_VARARGS, "bind_residual(addresses, version)"},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Calls into libaxo.so without ctypes.", -1, methods, NULL, NULL, NULL, NULL};

@@ -50,12 +50,53 @@ __global__ void __launch_bounds__(GATED_MAP_THREADS) gated_map_kernel(GatedMapAr
     });
 }
 
+// One value of a product with a residual: z = sum + bias.
+__device__ __forceinline__ void add_one(const GatedArgs& g, float z, int row, int col) {
+    const int64_t at = (int64_t)row * g.ldc + col, from = (int64_t)row * g.ldaux + col;
+    const float res = !g.aux ? 0.f : g.wide ? reinterpret_cast<const float*>(g.aux)[from] : bf16_bits_to_f32(g.aux[from]);
+    const float y = __builtin_fmaf(g.scale, apply_epilogue(z, 0.f, g.gate), res);
+    if (g.wide) reinterpret_cast<float*>(g.C)[at] = y;
+    else g.C[at] = f32_to_bf16_bits(y);
+    if (g.G) g.G[(int64_t)row * g.ldz + col] = f32_to_bf16_bits(z);
+}
+
+// dZ = scale dY act'(Z), element by element, eight columns of a row per thread and turn, as gated_map_kernel; without an activation dZ = scale dY, which
+// is then a rounding of the stream's gradient to what the products read.
+struct AddMapArgs {
+    const void* dY;
+    const bf16_t* Z;
+    bf16_t* dZ;
+    int64_t lddy, ldz, lddz;
+    int M, N, epilogue;
+    float scale;
+};
+template <typename T>
+__global__ void __launch_bounds__(GATED_MAP_THREADS) add_map_kernel(AddMapArgs g) {
+    const int64_t per_row = ((int64_t)g.N + 7) / 8, chunks = per_row * g.M, step = (int64_t)gridDim.x * GATED_MAP_THREADS;
+    with_act(g.epilogue, [&](auto act) __attribute__((always_inline)) {
+        constexpr int ACT = decltype(act)::value;
+        for (int64_t at = (int64_t)blockIdx.x * GATED_MAP_THREADS + threadIdx.x; at < chunks; at += step) {
+            const int64_t row = at / per_row, col = (at - row * per_row) * 8;
+            const int valid = (int)min((int64_t)8, g.N - col);
+            float d[8], z[8];
+            load_chunk(static_cast<const T*>(g.dY) + row * g.lddy + col, valid, d);
+            if (ACT != EPI_BIAS) load_chunk(g.Z + row * g.ldz + col, valid, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[i] *= g.scale;
+                if (ACT != EPI_BIAS) d[i] *= gate_both<ACT == EPI_BIAS_GELU_TANH ? GATE_GELU_TANH : GATE_GELU_ERF>(z[i]).y;
+            }
+            store_chunk(g.dZ + row * g.lddz + col, valid, d);
+        }
+    });
+}
+
 // The block's products for any sizes and spans, 64-bit indices, 128 x 128 tiles staged through registers as gemm_generic_kernel: what is left to it are
 // empty reductions, operands whose spans pass 4 GiB and outputs of a billion rows or columns, whose 256-row tiles are too many for a launch.  Forward
-// 4096 x 8192 x 16384 12.7 ms, an eighth of the tiles' rate.
+// 4096 x 8192 x 16384 12.7 ms, an eighth of the tiles' rate.  (FC_ADD, the product with a residual, has the same kernels.)
 template <int OP>
 __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
-    constexpr int LB = OP == GATED_FWD ? MC : KC, SUMS = OP == GATED_FWD ? 2 : 1;
+    constexpr int LB = OP == GATED_FWD || OP == FC_ADD ? MC : KC, SUMS = OP == GATED_FWD ? 2 : 1;
     __shared__ __attribute__((aligned(16))) bf16_t As[GEN_BM * GEN_LDS_STRIDE];
     __shared__ __attribute__((aligned(16))) bf16_t Bs[SUMS][GEN_BN * GEN_LDS_STRIDE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
@@ -95,6 +136,22 @@ __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
     };
     walk(g.A, g.B);
     if constexpr (OP == GATED_DX) walk(g.A2, g.B2);
+    if constexpr (OP == FC_ADD) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int col = j0 + wn * 64 + b * 32 + (lane & 31);
+                if (col >= g.No) continue;
+                const float bias = g.bias ? bf16_bits_to_f32(g.bias[col]) : 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = i0 + wm * 64 + a * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                    if (row < g.Mo) add_one(g, acc[0][a][b][e] + bias, row, col);
+                }
+            }
+        return;
+    }
     // accumulator element e of a 32x32 tile: row 8*(e/4) + 4*(lane/32) + e%4, column lane%32
     with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
         constexpr int GATE = decltype(gate)::value;
@@ -138,7 +195,7 @@ __global__ void __launch_bounds__(256) gated_generic_kernel(GatedArgs g) {
 // 735 us: the rest is G and U read and a second output, which no reduction hides, since all tiles of a round come to their ends together); dX of 4096 x 7168 x 14336
 // 1.29 ms, 1310.  1001 x 1027 x 515 forward 10.1 us, through the activation 9.0.
 template <int OP>
-constexpr int GATED_LB = OP == GATED_FWD ? MC : KC;
+constexpr int GATED_LB = OP == GATED_FWD || OP == FC_ADD ? MC : KC;
 template <int OP>
 constexpr int gated_cols(int BN) { return OP == GATED_FWD ? BN / 2 : BN; }  // of the output, in a tile of BN columns of B
 

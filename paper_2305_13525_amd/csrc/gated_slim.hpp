@@ -45,6 +45,16 @@ __device__ __forceinline__ void gated_finish(const GatedArgs& g, const f32x4 (&s
         store_bf16_quad(h, v, row, col, valid);
     };
     if constexpr (OP == GATED_DX || OP == GATED_DW) store(g.C, g.ldc, sum[0]);
+    else if constexpr (OP == FC_ADD)
+        with_act(g.gate, [&](auto act) __attribute__((always_inline)) {
+            const f32x4 z = sum[0] + x1;
+            f32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(g.scale, apply_epilogue(z[e], 0.f, decltype(act)::value), x2[e]);
+            if (g.wide) store_f32_quad(g, y, row, col, valid);
+            else store(g.C, g.ldc, y);
+            if (g.G) store(g.G, g.ldz, z);
+        });
     else
         with_gate(g.gate, [&](auto gate) __attribute__((always_inline)) {
             constexpr int GATE = decltype(gate)::value;
@@ -70,10 +80,19 @@ __device__ __forceinline__ void gated_finish(const GatedArgs& g, const f32x4 (&s
         });
 }
 
+// The bias and the residual of four columns of a row, `valid` (0 and less: none) of them inside the matrix.
+__device__ __forceinline__ void add_extras(const GatedArgs& g, int row, int col, int valid, f32x4& bias, f32x4& res) {
+    bias = res = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (g.bias) bias = load_bf16x4(g.bias + col, valid);
+    if (!g.aux) return;
+    const int64_t at = (int64_t)row * g.ldaux + col;
+    res = g.wide ? load_f32x4(reinterpret_cast<const float*>(g.aux) + at, valid) : load_bf16x4(g.aux + at, valid);
+}
+
 template <int OP, int BM, int BC, int NW, int ST>
 __global__ void __launch_bounds__(NW * 64) gated_slim_kernel(GatedProduct<OP> g, GatedSlimSched sc) {
     using C = GatedSlimCfg<OP, BM, BC, NW, ST>;
-    constexpr int LB = OP == GATED_FWD ? MC : KC;
+    constexpr int LB = OP == GATED_FWD || OP == FC_ADD ? MC : KC;
     using OA = SlimOperand<BM, KC>;
     using OB = SlimOperand<BC, LB>;
     constexpr int TM = BM / 16, TN = BC / 16, PARTS = C::PARTS;
@@ -95,7 +114,7 @@ __global__ void __launch_bounds__(NW * 64) gated_slim_kernel(GatedProduct<OP> g,
     a_rsrc[0] = tile_rsrc(OA::origin(g.A, g.lda, i0), a_bound);
     b_rsrc[0] = tile_rsrc(OB::origin(g.B, g.ldb, j0), b_bound);
     if constexpr (OP == GATED_DX) a_rsrc[1] = tile_rsrc(OA::origin(g.A2, g.lda, i0), a_bound);
-    if constexpr (OP != GATED_DACT) b_rsrc[1] = tile_rsrc(OB::origin(g.B2, g.ldb, j0), b_bound);
+    if constexpr (OP == GATED_FWD || OP == GATED_DX) b_rsrc[1] = tile_rsrc(OB::origin(g.B2, g.ldb, j0), b_bound);
     const uint32_t a_step = OA::chunk_step(g.lda), b_step = OB::chunk_step(g.ldb);
     char* const mine = smem + wave * C::WAVE_BYTES;
     const uint32_t mine_lds = (uint32_t)(uintptr_t)(lds_void_ptr)smem + wave * C::WAVE_BYTES;
@@ -189,7 +208,13 @@ __global__ void __launch_bounds__(NW * 64) gated_slim_kernel(GatedProduct<OP> g,
         x = f32x4{0.f, 0.f, 0.f, 0.f};
         if (p) x = load_bf16x4(OP == GATED_FWD ? p + col : p + (int64_t)row * g.ldaux + col, valid);
     };
-    if constexpr (OP != GATED_DX)
+    if constexpr (OP == FC_ADD)
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int row = i0 + quad_row(i), col = j0 + quad_col(i);
+            add_extras(g, row, col, quad_row(i) < BM && row < g.Mo ? g.No - col : 0, x1[i], x2[i]);
+        }
+    else if constexpr (OP != GATED_DX)
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i) {
             extras(OP == GATED_FWD ? g.bias : g.aux, x1[i], i);
@@ -296,7 +321,7 @@ __device__ __forceinline__ void split_tile(const GatedSplitSched& sc, int tile, 
 template <int OP, bool LINES>
 __global__ void __launch_bounds__(TILE_THREADS, 1) gated_split_kernel(GatedProduct<OP> product, GatedSplitSched sc) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    constexpr int LA = OP == GATED_DW ? MC : KC, LB = OP == GATED_FWD || OP == GATED_DW ? MC : KC;
+    constexpr int LA = OP == GATED_DW ? MC : KC, LB = OP == GATED_FWD || OP == GATED_DW || OP == FC_ADD ? MC : KC;
     const int id = xcd_run(blockIdx.x, gridDim.x), tiles = sc.tiles_m * sc.tiles_n, tile = id % tiles, slice = id / tiles;
     GatedSlice<OP> g;
     static_cast<GatedProduct<OP>&>(g) = product;
@@ -328,6 +353,7 @@ __global__ void __launch_bounds__(SPLIT_JOIN_THREADS) gated_split_join_kernel(Ga
         if (g.bias) x1 = load_bf16x4(g.bias + col, valid);
         if (g.bias2) x2 = load_bf16x4(g.bias2 + col, valid);
     }
+    if constexpr (OP == FC_ADD) add_extras(g, row, col, valid, x1, x2);
     if constexpr (OP == GATED_DACT) {
         x1 = load_bf16x4(g.aux + (int64_t)row * g.ldaux + col, valid);
         x2 = load_bf16x4(g.aux2 + (int64_t)row * g.ldaux + col, valid);

@@ -1073,6 +1073,120 @@ __device__ __forceinline__ void gated_dact_epilogue(const Args& g, f32x4 (&acc)[
     });
 }
 
+// The act(sum + bias) of a forward product with a residual, its kind as a compile-time constant.
+template <typename F>
+__device__ __forceinline__ void with_act(int epilogue, F f) {
+    if (epilogue == EPI_BIAS_GELU_TANH) f(IC<EPI_BIAS_GELU_TANH>{});
+    else if (epilogue == EPI_BIAS_GELU_ERF) f(IC<EPI_BIAS_GELU_ERF>{});
+    else f(IC<EPI_BIAS>{});
+}
+
+// A product added to a residual, C = R + scale act(sum + bias).  As gated_dact_epilogue: a wave stages its sums in fp32, a lane then holds eight columns of a row, reads the
+// residual and stores the result 16 bytes at a time (twice, of an fp32 stream), what a pass reads being requested two passes ahead.
+template <typename C, bool PLAIN, typename Args>
+__device__ __forceinline__ void add_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int wrow0, const int wcol0, const int wave, const int lane, char* smem,
+                                             const bool whole) {
+    constexpr int F_STRIDE = C::WTN * 4 + 16, ROWS = C::TM * C::TN == 32 ? 16 : 32, LPR = C::WTN / 8, RPI = 64 / LPR, ITERS = ROWS / RPI, PASSES = C::WTM / ROWS;
+    static_assert(C::WAVES * ROWS * F_STRIDE <= C::LDS_BYTES && ROWS % RPI == 0 && PASSES <= 8, "fits the operand buffers");
+    char* const stage = smem + wave * (ROWS * F_STRIDE);
+    const int lr = lane / LPR, lc = lane % LPR * 8, col = wcol0 + lc, valid = g.No - col;
+    f32x4 bias[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if (g.bias) {
+        bias[0] = load_bf16x4(g.bias + col, valid);
+        bias[1] = load_bf16x4(g.bias + col + 4, valid - 4);
+    }
+    auto of_type = [&](auto wide_tag) __attribute__((always_inline)) {
+        constexpr bool WIDE = decltype(wide_tag)::value;
+        using T = std::conditional_t<WIDE, float, bf16_t>;
+        constexpr int AHEAD = 2, N = WIDE ? 2 : 1;  // passes; 16-byte words of a lane's eight values
+        u32x4 rs[AHEAD + 1][ITERS][N];
+        auto request = [&](auto pass_tag) __attribute__((always_inline)) {
+            constexpr int pass = decltype(pass_tag)::value, s = pass % (AHEAD + 1);
+#pragma unroll
+            for (int i = 0; i < ITERS; ++i) {
+                const int row = wrow0 + pass * ROWS + i * RPI + lr;
+                const T* const from = reinterpret_cast<const T*>(g.aux) + (int64_t)row * g.ldaux + col;
+                if (g.aux && (whole || (row < g.Mo && valid >= 8))) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) rs[s][i][n] = reinterpret_cast<const u32x4*>(from)[n];
+                } else {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) rs[s][i][n] = u32x4{0u, 0u, 0u, 0u};
+                    if (g.aux && row < g.Mo)
+#pragma unroll
+                        for (int e = 0; e < 7; ++e)
+                            if (e < valid) {
+                                if constexpr (WIDE) rs[s][i][e / 4][e % 4] = __float_as_uint(from[e]);
+                                else rs[s][i][0][e / 2] |= (uint32_t)from[e] << (e % 2 * 16);
+                            }
+                }
+            }
+        };
+        request(IC<0>{});
+        __syncthreads();  // all waves are done reading the operand buffers
+        with_act(g.gate, [&](auto act) __attribute__((always_inline)) {
+            auto pass = [&](auto p_tag) __attribute__((always_inline)) {
+                constexpr int p = decltype(p_tag)::value, s = p % (AHEAD + 1);
+                if constexpr (p >= PASSES) return;
+                else {
+#pragma unroll
+                for (int a = 0; a < ROWS / 16; ++a)
+#pragma unroll
+                    for (int b = 0; b < C::TN; ++b)
+                        *reinterpret_cast<f32x4*>(stage + (a * 16 + (lane & 15)) * F_STRIDE + (b * 16 + 4 * (lane >> 4)) * 4) = acc[p * (ROWS / 16) + a][b];
+                // behind the staging, which frees the registers of the sums
+                if constexpr (p == 0 && PASSES > 1) request(IC<1>{});
+                if constexpr (p + AHEAD < PASSES) request(IC<p + AHEAD>{});
+                __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the region is private to the wave
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int i = 0; i < ITERS; ++i) {
+                    const int r = i * RPI + lr, row = wrow0 + p * ROWS + r;
+                    f32x4 z[2], y[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        z[h] = *reinterpret_cast<const f32x4*>(stage + r * F_STRIDE + lc * 4 + h * 16) + bias[h];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float res = WIDE ? __uint_as_float(rs[s][i][N - 1 == 0 ? 0 : h][e])
+                                                   : __uint_as_float(e % 2 ? rs[s][i][0][h * 2 + e / 2] & 0xFFFF0000u : rs[s][i][0][h * 2 + e / 2] << 16);
+                            y[h][e] = __builtin_fmaf(g.scale, apply_epilogue(z[h][e], 0.f, decltype(act)::value), res);
+                        }
+                    }
+                    if (whole || (row < g.Mo && valid > 0)) {
+                        T* const to = reinterpret_cast<T*>(g.C) + (int64_t)row * g.ldc + col;
+                        if constexpr (!WIDE)
+                            store_eight<PLAIN>(u32x4{pack_bf16x2(y[0][0], y[0][1]), pack_bf16x2(y[0][2], y[0][3]), pack_bf16x2(y[1][0], y[1][1]), pack_bf16x2(y[1][2], y[1][3])},
+                                               to, whole, valid);
+                        else if (whole || valid >= 8) {
+                            store_row<PLAIN>(__builtin_bit_cast(u32x4, y[0]), reinterpret_cast<u32x4*>(to));
+                            store_row<PLAIN>(__builtin_bit_cast(u32x4, y[1]), reinterpret_cast<u32x4*>(to) + 1);
+                        } else
+#pragma unroll
+                            for (int e = 0; e < 7; ++e)
+                                if (e < valid) to[e] = y[e / 4][e % 4];
+                        if (g.G)
+                            store_eight<PLAIN>(u32x4{pack_bf16x2(z[0][0], z[0][1]), pack_bf16x2(z[0][2], z[0][3]), pack_bf16x2(z[1][0], z[1][1]), pack_bf16x2(z[1][2], z[1][3])},
+                                               g.G + (int64_t)row * g.ldz + col, whole, valid);
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();  // LDS operations of a wave complete in order: the next pass may overwrite
+                }
+            };
+            pass(IC<0>{});
+            pass(IC<1>{});
+            pass(IC<2>{});
+            pass(IC<3>{});
+            pass(IC<4>{});
+            pass(IC<5>{});
+            pass(IC<6>{});
+            pass(IC<7>{});
+        });
+    };
+    if (g.wide) of_type(std::true_type{});
+    else of_type(std::false_type{});
+}
+
 // One BM x BN output tile with its top-left corner at (i0, j0), whole reduction.  LINES: the rows of A, which is KC, are
 // fetched by whole cache lines (line_phase), on three stages; with them and two of B the LDS is full, so rows of B that
 // do not start on lines still put every segment into two.  The loads of a step then touch 768 lines (dgrad) or 576 (forward) instead
@@ -1167,7 +1281,7 @@ __device__ __forceinline__ void gemm_tile_body(const Args& g, const int i0, cons
 #pragma unroll
             for (int b = 0; b < C::TN; ++b)
                 acc[ah * C::AH + a][b] =
-                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[bset][b], fa[aset][a], acc[ah * C::AH + a][b], 0, 0, 0);
+                    mfma_16x16x32<Args::F16>(fb[bset][b], fa[aset][a], acc[ah * C::AH + a][b]);
     };
     constexpr int N_MFMA = C::AH * C::TN;
     constexpr int RD_A = (LA == KC ? 1 : 2) * C::AH, RD_B = (LB == KC ? 1 : 2) * C::TN;
@@ -1361,8 +1475,10 @@ __device__ __forceinline__ void gemm_tile_body(const Args& g, const int i0, cons
     step(1, T1{}, false, false, false, false);
     AXO_SETPRIO(0);
 
-    if constexpr (Args::OP == GATED_FWD) gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
+    if constexpr (Args::OWN) Args::template finish<C, BM, BN>(g, acc, i0, j0, wm, wn, tid, smem);
+    else if constexpr (Args::OP == GATED_FWD) gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
     else if constexpr (Args::OP == GATED_DACT) gated_dact_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, i0 + BM <= g.Mo && j0 + BN <= g.No);
+    else if constexpr (Args::OP == FC_ADD) add_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, i0 + BM <= g.Mo && j0 + BN <= g.No);
     else if (i0 + BM <= g.Mo && j0 + BN <= g.No) tile_epilogue<C, LA, LB, PLAIN>(g, acc, i0, j0, wave, wm, wn, lane, smem);
     else tile_epilogue_clipped<C, LA, LB>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem);
 }
@@ -1455,7 +1571,7 @@ __device__ __forceinline__ void gemm_ring_body(const Args& g, const int i0, cons
         for (int a = 0; a < C::TM; ++a)
 #pragma unroll
             for (int b = 0; b < C::TN; ++b)
-                acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kq][b], fa[kq][a], acc[a][b], 0, 0, 0);
+                acc[a][b] = mfma_16x16x32<Args::F16>(fb[kq][b], fa[kq][a], acc[a][b]);
     };
     constexpr int N_MFMA = C::TM * C::TN, RD = (LA == KC ? 1 : 2) * C::TM + (LB == KC ? 1 : 2) * C::TN;
     constexpr int NL = C::A_ROUNDS + C::B_ROUNDS;
@@ -1542,7 +1658,7 @@ __device__ __forceinline__ void gemm_ring_body(const Args& g, const int i0, cons
     enum { EARLY, LATE, MIXED };
     constexpr bool SMALL = BM <= 128;
     constexpr int EPILOGUE = BM * BN < 128 * 128 || (LA == KC && LB == MC) ? EARLY : LB == KC ? MIXED : LATE;
-    constexpr bool OWN_EPILOGUE = Args::OP == GATED_FWD || Args::OP == GATED_DACT;
+    constexpr bool OWN_EPILOGUE = Args::OP == GATED_FWD || Args::OP == GATED_DACT || Args::OP == FC_ADD || Args::OWN;
     [[maybe_unused]] std::conditional_t<SMALL && !OWN_EPILOGUE, SmallEpilogue<C, LA, LB>, char> epilogue;
     if constexpr (SMALL && EPILOGUE == EARLY && !OWN_EPILOGUE) epilogue.request(g, i0 + wm * C::WTM, j0 + wn * C::WTN, lane);
     const int lead = KT % D, first = lead > 0 ? D - lead : 0;
@@ -1603,8 +1719,10 @@ __device__ __forceinline__ void gemm_ring_body(const Args& g, const int i0, cons
                 *reinterpret_cast<f32x4*>(g.partial + (wm * C::WTM + a * 16 + (lane & 15)) * BN + col + 4 * (lane >> 4)) = acc[a][b];
             }
         return;
-    } else if constexpr (Args::OP == GATED_FWD) return gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
+    } else if constexpr (Args::OWN) return Args::template finish<C, BM, BN>(g, acc, i0, j0, wm, wn, tid, smem);
+    else if constexpr (Args::OP == GATED_FWD) return gated_fwd_epilogue<C, BM, BN, PLAIN>(g, acc, i0, j0, wm, wn, tid, smem);
     else if constexpr (Args::OP == GATED_DACT) return gated_dact_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, whole);
+    else if constexpr (Args::OP == FC_ADD) return add_epilogue<C, PLAIN>(g, acc, i0 + wm * C::WTM, j0 + wn * C::WTN, wave, lane, smem, whole);
     else {
     if constexpr (!SMALL || EPILOGUE == MIXED)
         if (whole) return tile_epilogue<C, LA, LB, PLAIN>(g, acc, i0, j0, wave, wm, wn, lane, smem);
