@@ -14,34 +14,12 @@ using axo::bf16_t;
 
 inline int launched() { return hipGetLastError() == hipSuccess ? AXO_OK : AXO_ERR_HIP; }
 
-// How the symmetric products are cut: tiles of `size`, their steps in equal shares for `workgroups`.
-struct SymPlan {
-    int size = 64, workgroups = 0;
-    int tiles = 0;
-};
-constexpr int64_t SYM_MOST_SHARES = 12;  // workgroups to a tile: what the last one has to add up
-// A step of a 64 x 64 tile takes 0.235 us with a compute unit to itself and 0.15 where two run beside each other, one of 128 x 128 0.42; a share's
-// end and the addition of its tile's others some 3 us.
-SymPlan sym_plan(int64_t s, int64_t steps) {
-    auto of = [&](int size, int64_t most, SymPlan& plan) {
-        const int64_t n = tiles_in((int)s, size), tiles = n * (n + 1) / 2, units = tiles * steps;
-        plan.size = size;
-        plan.tiles = (int)tiles;
-        plan.workgroups = (int)std::min<int64_t>({units, most, SYM_MOST_SHARES * tiles});
-        return (double)((units + plan.workgroups - 1) / plan.workgroups);
-    };
-    SymPlan one, two, big;
-    const double t1 = of(64, NUM_CU, one) * 0.235, t2 = of(64, 2 * NUM_CU, two) * 0.30, t3 = of(128, NUM_CU, big) * 0.42 + 1.0;
-    if (t3 <= std::min(t1, t2)) return big;
-    return t1 <= t2 ? one : two;
-}
-
 // Everything that a call takes from its sizes.
 struct OrthoPlan {
     int64_t s, l;    // padded
     bool tall;       // more rows than columns
     int exponent;    // X is held as its values times 2^exponent
-    SymPlan gram, poly;
+    axo::SymPlan gram, poly;
     size_t counters, sums, A, Q, X[2], partial, bytes;  // offsets in the workspace
 };
 int make_plan(const Shard& sh, OrthoPlan* p) {
@@ -54,16 +32,16 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
     if ((p->l + 4 * axo::TILE_BK) * p->s * 2 >= (int64_t)0xFFFF0000) return AXO_ERR_BAD_SIZE;
     // about sqrt(K N), whose reciprocal is what the values of X come to; fp16 ends at 2^16, and they reach 2^exponent
     p->exponent = std::min(13, (int)std::floor(0.5 * std::log2((double)K * (double)N)));
-    p->gram = sym_plan(p->s, p->l / axo::TILE_BK);
-    p->poly = sym_plan(p->s, p->s / axo::TILE_BK);
+    p->gram = axo::sym_plan(p->s, p->l / axo::TILE_BK, NUM_CU);
+    p->poly = axo::sym_plan(p->s, p->s / axo::TILE_BK, NUM_CU);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t from = at;
         at += (bytes + 255) / 256 * 256;
         return from;
     };
-    auto partials = [](const SymPlan& y) { return (size_t)y.workgroups * 2 * y.size * y.size * sizeof(float); };
-    p->counters = take((size_t)std::max(p->gram.tiles, p->poly.tiles) * sizeof(uint32_t));
+    auto partials = [](const axo::SymPlan& y) { return (size_t)y.cut.slots() * y.size * y.size * sizeof(float); };
+    p->counters = take((size_t)std::max(p->gram.cut.cut, p->poly.cut.cut) * sizeof(uint32_t));
     p->sums = take(axo::ORTHO_SUMS * sizeof(double));
     p->A = take((size_t)(p->s * p->s) * 2);
     p->Q = take((size_t)(p->s * p->s) * 2);
@@ -75,21 +53,22 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
 
 template <int SIZE, int LAYOUT>
 int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
-    using C = std::conditional_t<SIZE == 64, axo::SmallCfg<false>, axo::MidCfg>;
+    using C = std::conditional_t<SIZE == 64, axo::SmallCfg<false>, std::conditional_t<SIZE == 128, axo::MidCfg, axo::MixBigCfg>>;
     auto kern = [] {
         if constexpr (SIZE == 64) return axo::ortho_sym_64_kernel<LAYOUT>;
-        else return axo::ortho_sym_128_kernel<LAYOUT>;
+        else if constexpr (SIZE == 128) return axo::ortho_sym_128_kernel<LAYOUT>;
+        else return axo::ortho_sym_256_kernel<LAYOUT>;
     }();
     static std::atomic<uint64_t> raised{0};
     if (!raise_lds_limit(reinterpret_cast<const void*>(kern), C::LDS_BYTES, &raised)) return AXO_ERR_HIP;
     hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(C::THREADS), C::LDS_BYTES, st, g);
     return launched();
 }
-int launch_sym(axo::OrthoSym g, const SymPlan& y, bool tall, hipStream_t st) {
-    g.steps = g.R / axo::TILE_BK;
-    g.tiles = y.tiles;
+int launch_sym(axo::OrthoSym g, const axo::SymPlan& y, bool tall, hipStream_t st) {
+    g.cut = y.cut;
     if (y.size == 64) return tall ? launch_sym<64, axo::MC>(g, y.workgroups, st) : launch_sym<64, axo::KC>(g, y.workgroups, st);
-    return tall ? launch_sym<128, axo::MC>(g, y.workgroups, st) : launch_sym<128, axo::KC>(g, y.workgroups, st);
+    if (y.size == 128) return tall ? launch_sym<128, axo::MC>(g, y.workgroups, st) : launch_sym<128, axo::KC>(g, y.workgroups, st);
+    return tall ? launch_sym<256, axo::MC>(g, y.workgroups, st) : launch_sym<256, axo::KC>(g, y.workgroups, st);
 }
 template <int LB>
 int launch_apply(const axo::OrthoApply& g, hipStream_t st) {

@@ -13,11 +13,12 @@
 #include "axo_common.hpp"
 #include "gemm_tile.hpp"
 #include "norm.hpp"
+#include "sym_cut.hpp"
 
 namespace axo {
 
 constexpr int ORTHO_PAD = 64;
-constexpr int ORTHO_SUMS = 256;  // workgroups that sum up G's squares
+constexpr int ORTHO_SUMS = 512;  // workgroups that sum up G's squares
 
 struct OrthoLoadArgs {
     const void* G; int64_t ldg;
@@ -44,12 +45,13 @@ __device__ __forceinline__ double ortho_block_sum(double v, double* lds) {
 template <typename T>
 __global__ void __launch_bounds__(ORTHO_THREADS) ortho_norm_kernel(OrthoLoadArgs g) {
     __shared__ double lds[ORTHO_THREADS / 64];
-    const int64_t per_row = ((int64_t)g.N + 7) / 8, chunks = per_row * g.K, step = (int64_t)gridDim.x * ORTHO_THREADS;
+    // (fewer than 2^28 chunks, of weights of fewer than 2^31 values)
+    const uint32_t per_row = ((uint32_t)g.N + 7) / 8, chunks = per_row * (uint32_t)g.K, step = gridDim.x * ORTHO_THREADS;
     double sum = 0.0;
-    for (int64_t at = (int64_t)blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += step) {
-        const int64_t row = at / per_row, col = (at - row * per_row) * 8;
+    for (uint32_t at = blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += step) {
+        const uint32_t row = at / per_row, col = (at - row * per_row) * 8;
         float v[8];
-        load_chunk(static_cast<const T*>(g.G) + row * g.ldg + col, (int)min((int64_t)8, g.N - col), v);
+        load_chunk(static_cast<const T*>(g.G) + (int64_t)row * g.ldg + col, min(8, g.N - (int)col), v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += (double)v[i] * (double)v[i];
     }
@@ -67,40 +69,33 @@ __global__ void __launch_bounds__(ORTHO_THREADS) ortho_load_kernel(OrthoLoadArgs
     __shared__ double lds[ORTHO_THREADS / 64];
     const double norm = sqrt(ortho_block_sum(threadIdx.x < ORTHO_SUMS ? g.sums[threadIdx.x] : 0.0, lds)) + (double)g.eps;
     const double factor = norm == 0.0 ? 0.0 : g.scale / norm;
-    const int64_t per_row = g.cols / 8, chunks = per_row * g.rows, step = (int64_t)gridDim.x * ORTHO_THREADS;
-    for (int64_t at = (int64_t)blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += step) {
-        const int64_t row = at / per_row, col = (at - row * per_row) * 8;
+    const uint32_t per_row = (uint32_t)g.cols / 8, chunks = per_row * (uint32_t)g.rows, step = gridDim.x * ORTHO_THREADS;
+    for (uint32_t at = blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += step) {
+        const uint32_t row = at / per_row, col = (at - row * per_row) * 8;
         u32x4 w = {0u, 0u, 0u, 0u};
-        if (row < g.K && col < g.N) {
+        if ((int)row < g.K && (int)col < g.N) {
             float v[8];
-            load_chunk(static_cast<const T*>(g.G) + row * g.ldg + col, (int)min((int64_t)8, g.N - col), v);
+            load_chunk(static_cast<const T*>(g.G) + (int64_t)row * g.ldg + col, min(8, g.N - (int)col), v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = pack_f16x2((float)((double)v[2 * i] * factor), (float)((double)v[2 * i + 1] * factor));
         }
-        *reinterpret_cast<u32x4*>(g.X + at * 8) = w;
+        *reinterpret_cast<u32x4*>(g.X + (int64_t)at * 8) = w;
     }
 }
 
 // ---- gram and poly ----------------------------------------------------------------------------
-// The tiles on and below the diagonal of a symmetric output, and their mirror images.  Their steps of the reduction are dealt out to the workgroups in equal, contiguous shares, so
-// that every workgroup has the same to do whatever the numbers: a share begins and ends inside a tile, and such a tile's sums are written to the workspace; whoever
-// comes last adds them up, in the order of the steps, and finishes the tile.  Which workgroup that is depends on timing, what it computes does not, and none waits for
-// another.  Those sums go past the L2 of an XCD by device-scope accesses.
+// The tiles on and below the diagonal of a symmetric output, and their mirror images, dealt out as sym_cut.hpp says.  (With every workgroup's share a contiguous run of
+// all tiles' steps, wherever that begins in a tile, 4096 x 4096 with reductions of 16384 took 570 us, 500 TFLOP/s: 256 compute units read 7.8 TB/s of operands from behind
+// the caches.)
+// A part of a tile leaves its sums in the workspace; whoever comes last adds them up, in the order of the steps, and finishes the tile.  Which workgroup that
+// is depends on timing, what it computes does not, and none waits for another.  Those sums go past the L2 of an XCD by device-scope accesses.
 struct OrthoSym : GemmArgs {
     static constexpr bool F16 = true, OWN = true;
     float alpha, beta, diag;   // C = alpha sum + beta aux + diag on the diagonal; aux nullptr: none
-    float* partial;            // [2 x workgroups][tile]
-    uint32_t* counters;        // one per tile, zero
-    int steps;                 // of a tile
-    int tiles;
-    // of the segment at hand
-    int tile, from, count;     // steps
-    int slot;
-
-    // The workgroup that has unit u of all `tiles * steps`, dealt out to W workgroups: workgroup w begins with unit floor(w U / W).
-    __device__ __forceinline__ int64_t units() const { return (int64_t)tiles * steps; }
-    __device__ __forceinline__ int64_t first_of(int64_t w) const { return w * units() / gridDim.x; }
-    __device__ __forceinline__ int owner_of(int64_t u) const { return (int)(((u + 1) * gridDim.x - 1) / units()); }
+    float* partial;            // [slots][tile]
+    uint32_t* counters;        // one per tile that is cut, zero
+    SymCut cut;
+    SymPart part;              // at hand
 
     template <typename C, int BM, int BN>
     static __device__ __forceinline__ void finish(const OrthoSym& g, f32x4 (&acc)[C::TM][C::TN], const int i0, const int j0, const int wm, const int wn, const int tid,
@@ -114,84 +109,96 @@ template <typename C, int BM, int BN>
 __device__ __forceinline__ void OrthoSym::finish(const OrthoSym& g, f32x4 (&acc)[C::TM][C::TN], const int i0, const int j0, const int wm, const int wn, const int tid,
                                                  char* smem) {
     static_assert(BM == BN, "mirror images");
-    constexpr int STRIDE = BN * 2 + 16, CPR = BN / 8, ROUNDS = BM * CPR / C::THREADS, TILE = BM * BN;
-    static_assert(2 * BM * STRIDE <= C::LDS_BYTES && BM * CPR % C::THREADS == 0, "both images in the operand buffers");
-    const int lane = tid & 63;
-    const int row = wm * C::WTM + (lane & 15), col = wn * C::WTN + 4 * (lane >> 4);
+    constexpr int TILE = BM * BN;
+    const int lane = tid & 63, wave = wm * (BN / C::WTN) + wn;
     __syncthreads();  // all waves are done reading the operand buffers
-    if (g.count < g.steps) {
+    if (g.part.cut >= 0) {
         // a lane's quads lie behind each other by thread, in rounds: whole lines of the workspace
         auto at = [&](int a, int b) __attribute__((always_inline)) { return ((a * C::TN + b) * C::THREADS + tid) * 16; };
-        const __amdgpu_buffer_rsrc_t mine = partial_buffer(g.partial + (int64_t)g.slot * TILE, TILE * 4);
+        const __amdgpu_buffer_rsrc_t mine = partial_buffer(g.partial + (int64_t)g.part.slot * TILE, TILE * 4);
 #pragma unroll
         for (int a = 0; a < C::TM; ++a)
 #pragma unroll
             for (int b = 0; b < C::TN; ++b) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[a][b]), mine, at(a, b), 0, DEVICE_SCOPE);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's sums have arrived where all XCDs see them
         __syncthreads();
-        const int64_t first_unit = (int64_t)g.tile * g.steps;
-        const int first = g.owner_of(first_unit), last = g.owner_of(first_unit + g.steps - 1);
         uint32_t* const arrived = reinterpret_cast<uint32_t*>(smem);
-        if (tid == 0) *arrived = __hip_atomic_fetch_add(g.counters + g.tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) *arrived = __hip_atomic_fetch_add(g.counters + g.part.cut, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
-        const bool finishes = *arrived == (uint32_t)(last - first);
+        const bool finishes = *arrived == (uint32_t)(g.part.parts - 1);
         __syncthreads();  // the word has been read
         if (!finishes) return;
-        // the first one's share of this tile is the last of its segments, the others' the first of theirs
-        const int head = 2 * first + (g.first_of(first) < first_unit ? 1 : 0);
-        for (int w = first; w <= last; ++w) {
-            const __amdgpu_buffer_rsrc_t part = partial_buffer(g.partial + (int64_t)(w == first ? head : 2 * w) * TILE, TILE * 4);
-            f32x4 v[C::TM][C::TN];
+        for (int part = 0; part < g.part.parts; ++part) {
+            const __amdgpu_buffer_rsrc_t from = partial_buffer(g.partial + (int64_t)g.cut.slot_of(g.part.cut, part) * TILE, TILE * 4);
+            constexpr int ROWS = C::TM * C::TN > 16 ? 2 : C::TM;  // registers for so many rows of quads at a time
 #pragma unroll
-            for (int a = 0; a < C::TM; ++a)
+            for (int a0 = 0; a0 < C::TM; a0 += ROWS) {
+                f32x4 v[ROWS][C::TN];
 #pragma unroll
-                for (int b = 0; b < C::TN; ++b) v[a][b] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at(a, b), 0, DEVICE_SCOPE));
+                for (int a = 0; a < ROWS; ++a)
 #pragma unroll
-            for (int a = 0; a < C::TM; ++a)
+                    for (int b = 0; b < C::TN; ++b) v[a][b] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at(a0 + a, b), 0, DEVICE_SCOPE));
 #pragma unroll
-                for (int b = 0; b < C::TN; ++b) acc[a][b] = w == first ? v[a][b] : acc[a][b] + v[a][b];
+                for (int a = 0; a < ROWS; ++a)
+#pragma unroll
+                    for (int b = 0; b < C::TN; ++b) acc[a0 + a][b] = part == 0 ? v[a][b] : acc[a0 + a][b] + v[a][b];
+            }
         }
-        if (tid == 0) __hip_atomic_store(g.counters + g.tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) __hip_atomic_store(g.counters + g.part.cut, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    char* const image = smem + BM * STRIDE;
-    const bool mirrored = i0 != j0;
+    // what becomes of the sums, in place
+    const int row0 = i0 + wm * C::WTM, col0 = j0 + wn * C::WTN, r = lane & 15, c = 4 * (lane >> 4);
 #pragma unroll
     for (int a = 0; a < C::TM; ++a)
 #pragma unroll
         for (int b = 0; b < C::TN; ++b) {
-            const int r = row + a * 16, c = col + b * 16;
+            const int row = row0 + a * 16 + r, col = col0 + b * 16 + c;
             f32x4 v = acc[a][b] * g.alpha;
-            if (g.aux && i0 + r < g.Mo && j0 + c < g.No) {
-                const uint2 raw = *reinterpret_cast<const uint2*>(g.aux + (int64_t)(i0 + r) * g.ldaux + j0 + c);
+            if (g.aux && row < g.Mo && col < g.No) {
+                const uint2 raw = *reinterpret_cast<const uint2*>(g.aux + (int64_t)row * g.ldaux + col);
                 const f16x2 lo = __builtin_bit_cast(f16x2, raw.x), hi = __builtin_bit_cast(f16x2, raw.y);
                 v[0] = __builtin_fmaf(g.beta, (float)lo[0], v[0]);
                 v[1] = __builtin_fmaf(g.beta, (float)lo[1], v[1]);
                 v[2] = __builtin_fmaf(g.beta, (float)hi[0], v[2]);
                 v[3] = __builtin_fmaf(g.beta, (float)hi[1], v[3]);
             }
-            if (!mirrored)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += r == c + e ? g.diag : 0.f;
-            const uint2 packed = {pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
-            *reinterpret_cast<uint2*>(smem + r * STRIDE + c * 2) = packed;
-            if (mirrored) {
-                *reinterpret_cast<uint16_t*>(image + c * STRIDE + r * 2) = (uint16_t)packed.x;
-                *reinterpret_cast<uint16_t*>(image + (c + 1) * STRIDE + r * 2) = (uint16_t)(packed.x >> 16);
-                *reinterpret_cast<uint16_t*>(image + (c + 2) * STRIDE + r * 2) = (uint16_t)packed.y;
-                *reinterpret_cast<uint16_t*>(image + (c + 3) * STRIDE + r * 2) = (uint16_t)(packed.y >> 16);
-            }
+            for (int e = 0; e < 4; ++e) v[e] += row == col + e ? g.diag : 0.f;
+            acc[a][b] = v;
         }
-    __syncthreads();
-    auto out = [&](const char* from, int r0, int c0) __attribute__((always_inline)) {
+    // the wave's part of the tile, and its mirror image, each staged in a region of the wave's own and stored by rows
+    constexpr int STRIDE = C::WTN * 2 + 16, IMAGE_STRIDE = C::WTM * 2 + 16;
+    constexpr int BYTES = C::WTM * STRIDE > C::WTN * IMAGE_STRIDE ? C::WTM * STRIDE : C::WTN * IMAGE_STRIDE;
+    static_assert(C::WAVES * BYTES <= C::LDS_BYTES, "fits the operand buffers");
+    char* const stage = smem + wave * BYTES;
+    auto out = [&](auto rows_tag, auto cols_tag, int r0, int c0) __attribute__((always_inline)) {
+        constexpr int ROWS = decltype(rows_tag)::value, COLS = decltype(cols_tag)::value, LPR = COLS / 8, RPP = 64 / LPR, PASSES = ROWS / RPP;
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the region is private to the wave
+        __builtin_amdgcn_wave_barrier();
+        u32x4 v[PASSES];
 #pragma unroll
-        for (int i = 0; i < ROUNDS; ++i) {
-            const int q = i * C::THREADS + tid, r = q / CPR, c = q % CPR * 8;
-            if (r0 + r < g.Mo && c0 + c < g.No)
-                *reinterpret_cast<u32x4*>(g.C + (int64_t)(r0 + r) * g.ldc + c0 + c) = *reinterpret_cast<const u32x4*>(from + r * STRIDE + c * 2);
-        }
+        for (int p = 0; p < PASSES; ++p) v[p] = *reinterpret_cast<const u32x4*>(stage + (p * RPP + lane / LPR) * (COLS * 2 + 16) + lane % LPR * 16);
+        const int row = r0 + lane / LPR, col = c0 + lane % LPR * 8;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p)
+            if (row + p * RPP < g.Mo && col < g.No) *reinterpret_cast<u32x4*>(g.C + (int64_t)(row + p * RPP) * g.ldc + col) = v[p];
+        __builtin_amdgcn_wave_barrier();  // LDS operations of a wave complete in order: the next pass may overwrite
     };
-    out(smem, i0, j0);
-    if (mirrored) out(image, j0, i0);
+#pragma unroll
+    for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+        for (int b = 0; b < C::TN; ++b)
+            *reinterpret_cast<uint2*>(stage + (a * 16 + r) * STRIDE + (b * 16 + c) * 2) = uint2{pack_f16x2(acc[a][b][0], acc[a][b][1]), pack_f16x2(acc[a][b][2], acc[a][b][3])};
+    out(IC<C::WTM>{}, IC<C::WTN>{}, row0, col0);
+    if (i0 == j0) return;
+#pragma unroll
+    for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+        for (int b = 0; b < C::TN; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<_Float16*>(stage + (b * 16 + c + e) * IMAGE_STRIDE + (a * 16 + r) * 2) = (_Float16)acc[a][b][e];
+    out(IC<C::WTN>{}, IC<C::WTM>{}, col0, row0);
 }
 
 // The tile of an index: rows one behind the other, up to the diagonal.
@@ -202,25 +209,20 @@ __device__ __forceinline__ void ortho_tile(int t, int& ti, int& tj) {
     tj = t - ti * (ti + 1) / 2;
 }
 template <int SIZE, int LAYOUT>
-__device__ __forceinline__ void ortho_sym(OrthoSym g, char* smem) {
-    const int bid = xcd_run(blockIdx.x, gridDim.x);  // neighbours share rows of tiles
-    const int64_t begin = g.first_of(bid), end = g.first_of(bid + 1);
-    const bf16_t *const A = g.A, *const B = g.B;
-    for (int64_t u = begin; u < end;) {
-        g.tile = (int)(u / g.steps);
-        g.from = (int)(u - (int64_t)g.tile * g.steps);
-        g.count = (int)min((int64_t)(g.steps - g.from), end - u);
-        g.slot = 2 * bid + (u > begin ? 1 : 0);
-        g.R = g.count * TILE_BK;
-        const int64_t skip = (int64_t)g.from * TILE_BK * (LAYOUT == KC ? 1 : g.lda);
-        g.A = A + skip;
-        g.B = B + skip;
+__device__ __forceinline__ void ortho_sym(const OrthoSym& args, char* smem) {
+    SymWalk walk(args.cut, xcd_run(blockIdx.x, gridDim.x), gridDim.x);  // neighbours share rows of tiles
+    OrthoSym g = args;
+    for (bool first = true; walk.next(args.cut, g.part); first = false) {
+        g.R = g.part.count * TILE_BK;
+        const int64_t skip = (int64_t)g.part.from * TILE_BK * (LAYOUT == KC ? 1 : g.lda);
+        g.A = args.A + skip;
+        g.B = args.B + skip;
         int ti, tj;
-        ortho_tile(g.tile, ti, tj);
-        if (u > begin) __syncthreads();  // the tile before has left LDS
+        ortho_tile(g.part.tile, ti, tj);
+        if (!first) __syncthreads();  // the tile before has left LDS
         if constexpr (SIZE == 64) gemm_ring_body<64, 64, 2, 2, 4, LAYOUT, LAYOUT>(g, ti * 64, tj * 64, smem, threadIdx.x);
-        else gemm_ring_body<128, 128, 4, 2, 4, LAYOUT, LAYOUT>(g, ti * 128, tj * 128, smem, threadIdx.x);
-        u += g.count;
+        else if constexpr (SIZE == 128) gemm_ring_body<128, 128, 4, 2, 4, LAYOUT, LAYOUT>(g, ti * 128, tj * 128, smem, threadIdx.x);
+        else gemm_tile_body<256, 256, 2, 4, LAYOUT, LAYOUT>(g, ti * 256, tj * 256, smem);
     }
 }
 template <int LAYOUT>
@@ -232,6 +234,11 @@ template <int LAYOUT>
 __global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_128_kernel(OrthoSym g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     ortho_sym<128, LAYOUT>(g, smem);
+}
+template <int LAYOUT>
+__global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_256_kernel(OrthoSym g) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    ortho_sym<256, LAYOUT>(g, smem);
 }
 
 // ---- apply --------------------------------------------------------------------------------------
