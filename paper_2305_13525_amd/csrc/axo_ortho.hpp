@@ -19,6 +19,7 @@ struct OrthoPlan {
     int64_t s, l;    // padded
     bool tall;       // more rows than columns
     int exponent;    // X is held as its values times 2^exponent
+    bool at_once;    // a step is one launch
     axo::SymPlan gram, poly;
     size_t counters, sums, A, Q, X[2], partial, bytes;  // offsets in the workspace
 };
@@ -34,6 +35,7 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
     p->exponent = std::min(13, (int)std::floor(0.5 * std::log2((double)K * (double)N)));
     p->gram = axo::sym_plan(p->s, p->l / axo::TILE_BK, NUM_CU);
     p->poly = axo::sym_plan(p->s, p->s / axo::TILE_BK, NUM_CU);
+    p->at_once = p->s <= 128 && p->s * p->l <= axo::ORTHO_STEP_MOST;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t from = at;
@@ -53,9 +55,10 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
 
 template <int SIZE, int LAYOUT>
 int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
-    using C = std::conditional_t<SIZE == 64, axo::SmallCfg<false>, std::conditional_t<SIZE == 128, axo::MidCfg, axo::MixBigCfg>>;
+    using C = std::conditional_t<SIZE == 32, axo::SlimCfg<32, 32, axo::SLIM_WAVES, 1>, std::conditional_t<SIZE == 64, axo::SmallCfg<false>, std::conditional_t<SIZE == 128, axo::MidCfg, axo::MixBigCfg>>>;
     auto kern = [] {
-        if constexpr (SIZE == 64) return axo::ortho_sym_64_kernel<LAYOUT>;
+        if constexpr (SIZE == 32) return axo::ortho_sym_32_kernel<LAYOUT>;
+        else if constexpr (SIZE == 64) return axo::ortho_sym_64_kernel<LAYOUT>;
         else if constexpr (SIZE == 128) return axo::ortho_sym_128_kernel<LAYOUT>;
         else return axo::ortho_sym_256_kernel<LAYOUT>;
     }();
@@ -66,6 +69,7 @@ int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
 }
 int launch_sym(axo::OrthoSym g, const axo::SymPlan& y, bool tall, hipStream_t st) {
     g.cut = y.cut;
+    if (y.size == 32) return tall ? launch_sym<32, axo::MC>(g, y.workgroups, st) : launch_sym<32, axo::KC>(g, y.workgroups, st);
     if (y.size == 64) return tall ? launch_sym<64, axo::MC>(g, y.workgroups, st) : launch_sym<64, axo::KC>(g, y.workgroups, st);
     if (y.size == 128) return tall ? launch_sym<128, axo::MC>(g, y.workgroups, st) : launch_sym<128, axo::KC>(g, y.workgroups, st);
     return tall ? launch_sym<256, axo::MC>(g, y.workgroups, st) : launch_sym<256, axo::KC>(g, y.workgroups, st);
@@ -92,6 +96,15 @@ int launch_apply(const axo::OrthoApply& g, hipStream_t st) {
     return launched();
 }
 
+template <int S, int LAYOUT>
+int launch_step(const axo::OrthoStep& g, hipStream_t st) {
+    using C = std::conditional_t<S == 64, axo::SmallCfg<false>, axo::MidCfg>;
+    auto kern = axo::ortho_step_kernel<S, LAYOUT>;
+    static std::atomic<uint64_t> raised{0};
+    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), C::LDS_BYTES, &raised)) return AXO_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.R / 64)), dim3(C::THREADS), C::LDS_BYTES, st, g);
+    return launched();
+}
 template <typename T>
 int launch_load(const axo::OrthoLoadArgs& g, hipStream_t st) {
     hipLaunchKernelGGL(axo::ortho_norm_kernel<T>, dim3(axo::ORTHO_SUMS), dim3(axo::ORTHO_THREADS), 0, st, g);
@@ -119,6 +132,26 @@ int ortho(const OrthoPlan& pl, const axo::OrthoLoadArgs& from, int type, int ste
     for (int i = 0; i < steps; ++i) {
         const float* const c = abc ? abc + 3 * i : QUINTIC;
         const bf16_t* const x = X[i % 2];
+        if (pl.at_once) {
+            axo::OrthoStep y{};
+            y.A = y.B = x;
+            y.lda = y.ldb = load.cols;
+            y.C = X[(i + 1) % 2]; y.ldc = load.cols;
+            y.Mo = y.No = s; y.R = l;
+            y.alpha = (float)std::ldexp(1.0, -2 * pl.exponent);
+            y.a = c[0]; y.b = c[1]; y.c = c[2];
+            y.scale = (float)std::ldexp(1.0, -pl.exponent);
+            y.K = from.K; y.N = from.N;
+            y.tall = pl.tall;
+            if (i == steps - 1) {
+                y.O = O;
+                y.ldo = ldo;
+            }
+            if (const int rc = s == 64 ? (pl.tall ? launch_step<64, axo::MC>(y, st) : launch_step<64, axo::KC>(y, st))
+                                       : (pl.tall ? launch_step<128, axo::MC>(y, st) : launch_step<128, axo::KC>(y, st)))
+                return rc;
+            continue;
+        }
         axo::OrthoSym y{};
         y.A = y.B = x;
         y.lda = y.ldb = load.cols;

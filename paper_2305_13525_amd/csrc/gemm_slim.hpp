@@ -103,8 +103,9 @@ struct SlimCfg {
 };
 
 // One tile; tid: 0 .. NW * 64 - 1 among the threads that work on it.  Holds exactly one workgroup barrier.
-template <int BM, int BN, int NW, int ST, int LA, int LB>
-__device__ __forceinline__ void slim_tile_body(const GemmArgs& g, const int i0, const int j0, const int tid, char* smem) {
+// Args::OWN: Args::request(g, row, col) is what a quad of outputs reads, requested ahead of the reduction, Args::quad(g, i0 != j0, row, col, sum, that) finishes it.
+template <int BM, int BN, int NW, int ST, int LA, int LB, typename Args = GemmArgs>
+__device__ __forceinline__ void slim_tile_body(const Args& g, const int i0, const int j0, const int tid, char* smem) {
     using C = SlimCfg<BM, BN, NW, ST>;
     using OA = SlimOperand<BM, LA>;
     using OB = SlimOperand<BN, LB>;
@@ -183,7 +184,7 @@ __device__ __forceinline__ void slim_tile_body(const GemmArgs& g, const int i0, 
             for (int a = 0; a < TM; ++a)
 #pragma unroll
                 for (int b = 0; b < TN; ++b)
-                    acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kq][b], fa[kq][a], acc[a][b], 0, 0, 0);
+                    acc[a][b] = mfma_16x16x32<Args::F16>(fb[kq][b], fa[kq][a], acc[a][b]);
     };
     if (wave < KT) issue(0, wave);
     if (ST == 2 && wave + NW < KT) issue(1, wave + NW);
@@ -200,7 +201,13 @@ __device__ __forceinline__ void slim_tile_body(const GemmArgs& g, const int i0, 
     constexpr bool FWD = LA == KC && LB == MC, DGRAD = LA == KC && LB == KC;
     const bool has_extra = FWD ? g.epilogue != EPI_NONE && g.add_bias : g.epilogue != EPI_NONE;
     u32x4 early[ROUNDS];  // four bf16 values in the first two dwords, or four fp32 ones
-    if (has_extra) {
+    if constexpr (Args::OWN) {
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const uint2 raw = Args::request(g, i0 + quad_row(i), j0 + quad_col(i));
+            early[i] = u32x4{raw.x, raw.y, 0u, 0u};
+        }
+    } else if (has_extra) {
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i) {
             const int row = i0 + quad_row(i), col = j0 + quad_col(i);
@@ -245,6 +252,11 @@ __device__ __forceinline__ void slim_tile_body(const GemmArgs& g, const int i0, 
             if (row < g.Mo && col < g.No) store(i, row, col, min(4, g.No - col), sum);
         }
     };
+    if constexpr (Args::OWN)
+        return each_quad([&](int i, int row, int col, int, f32x4 sum) __attribute__((always_inline)) {
+            Args::quad(g, i0 != j0, row, col, sum, uint2{early[i][0], early[i][1]});
+        });
+    else {
     // The kind is decided once, ahead of the quads, and a product compiles only its own kinds: little code, which a short kernel fetches
     // while it runs it.
     auto plain = [&]() __attribute__((always_inline)) {
@@ -278,6 +290,7 @@ __device__ __forceinline__ void slim_tile_body(const GemmArgs& g, const int i0, 
             if (valid < 4) x = load_f32x4(reinterpret_cast<const float*>(g.C) + (int64_t)row * g.ldc + col, valid);
             store_f32_quad(g, x + sum, row, col, valid);
         });
+    }
     }
 }
 

@@ -11,6 +11,7 @@
 // All matrices here are padded with zeros to whole multiples of 64, so that inside no product has an edge within a chunk of eight; the padding stays zero.
 #pragma once
 #include "axo_common.hpp"
+#include "gemm_slim.hpp"
 #include "gemm_tile.hpp"
 #include "norm.hpp"
 #include "sym_cut.hpp"
@@ -97,6 +98,19 @@ struct OrthoSym : GemmArgs {
     SymCut cut;
     SymPart part;              // at hand
 
+    // Quads of outputs (gemm_slim.hpp): the four values of aux, and what becomes of their sums, stored in both places.
+    static __device__ __forceinline__ uint2 request(const OrthoSym& g, int row, int col) {
+        return g.aux && row < g.Mo && col < g.No ? *reinterpret_cast<const uint2*>(g.aux + (int64_t)row * g.ldaux + col) : uint2{0u, 0u};
+    }
+    __device__ __forceinline__ f32x4 value(int row, int col, f32x4 sum, uint2 raw) const {
+        const f16x2 lo = __builtin_bit_cast(f16x2, raw.x), hi = __builtin_bit_cast(f16x2, raw.y);
+        const float x[4] = {(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(beta, x[e], sum[e] * alpha) + (row == col + e ? diag : 0.f);
+        return sum;
+    }
+    static __device__ __forceinline__ void quad(const OrthoSym& g, bool mirrored, int row, int col, f32x4 sum, uint2 raw);
+
     template <typename C, int BM, int BN>
     static __device__ __forceinline__ void finish(const OrthoSym& g, f32x4 (&acc)[C::TM][C::TN], const int i0, const int j0, const int wm, const int wn, const int tid,
                                                   char* smem);
@@ -153,18 +167,7 @@ __device__ __forceinline__ void OrthoSym::finish(const OrthoSym& g, f32x4 (&acc)
 #pragma unroll
         for (int b = 0; b < C::TN; ++b) {
             const int row = row0 + a * 16 + r, col = col0 + b * 16 + c;
-            f32x4 v = acc[a][b] * g.alpha;
-            if (g.aux && row < g.Mo && col < g.No) {
-                const uint2 raw = *reinterpret_cast<const uint2*>(g.aux + (int64_t)row * g.ldaux + col);
-                const f16x2 lo = __builtin_bit_cast(f16x2, raw.x), hi = __builtin_bit_cast(f16x2, raw.y);
-                v[0] = __builtin_fmaf(g.beta, (float)lo[0], v[0]);
-                v[1] = __builtin_fmaf(g.beta, (float)lo[1], v[1]);
-                v[2] = __builtin_fmaf(g.beta, (float)hi[0], v[2]);
-                v[3] = __builtin_fmaf(g.beta, (float)hi[1], v[3]);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += row == col + e ? g.diag : 0.f;
-            acc[a][b] = v;
+            acc[a][b] = g.value(row, col, acc[a][b], request(g, row, col));
         }
     // the wave's part of the tile, and its mirror image, each staged in a region of the wave's own and stored by rows
     constexpr int STRIDE = C::WTN * 2 + 16, IMAGE_STRIDE = C::WTM * 2 + 16;
@@ -201,6 +204,14 @@ __device__ __forceinline__ void OrthoSym::finish(const OrthoSym& g, f32x4 (&acc)
     out(IC<C::WTN>{}, IC<C::WTM>{}, col0, row0);
 }
 
+__device__ __forceinline__ void OrthoSym::quad(const OrthoSym& g, bool mirrored, int row, int col, f32x4 sum, uint2 raw) {
+    const f32x4 v = g.value(row, col, sum, raw);
+    *reinterpret_cast<uint2*>(g.C + (int64_t)row * g.ldc + col) = uint2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+    if (!mirrored) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<_Float16*>(g.C + (int64_t)(col + e) * g.ldc + row) = (_Float16)v[e];
+}
+
 // The tile of an index: rows one behind the other, up to the diagonal.
 __device__ __forceinline__ void ortho_tile(int t, int& ti, int& tj) {
     ti = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
@@ -225,6 +236,14 @@ __device__ __forceinline__ void ortho_sym(const OrthoSym& args, char* smem) {
         else gemm_tile_body<256, 256, 2, 4, LAYOUT, LAYOUT>(g, ti * 256, tj * 256, smem);
     }
 }
+// 32 x 32 tiles whose waves split the reduction, for outputs of few tiles.
+template <int LAYOUT>
+__global__ void __launch_bounds__(SLIM_WAVES * 64) ortho_sym_32_kernel(OrthoSym g) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    int ti, tj;
+    ortho_tile(xcd_run(blockIdx.x, gridDim.x), ti, tj);
+    slim_tile_body<32, 32, SLIM_WAVES, 1, LAYOUT, LAYOUT>(g, ti * 32, tj * 32, threadIdx.x, smem);
+}
 template <int LAYOUT>
 __global__ void __launch_bounds__(256, 2) ortho_sym_64_kernel(OrthoSym g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -239,6 +258,153 @@ template <int LAYOUT>
 __global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_256_kernel(OrthoSym g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     ortho_sym<256, LAYOUT>(g, smem);
+}
+
+// ---- a step in one launch ----------------------------------------------------------------------
+// Where s is at most 128 the three products of a step are too small to be worth a launch each: 3 to 4 us apiece, of which the matrix units work a tenth.  A workgroup here
+// has a slab of 64 of the l columns (rows, of a tall X) of the next X, and forms the whole of A for itself, as one tile of S x S; A, Q and the slab of X then go through LDS
+// only.  Every workgroup does the same l / 64 steps of A, so this is for X of up to ORTHO_STEP_MOST values.  Five steps with three launches each and with one: 128 x 512 65 and 48 us,
+// 128 x 2048 some 75 and 84.
+constexpr int ORTHO_STEP_MOST = 128 * 1024;
+struct OrthoStep : GemmArgs {
+    static constexpr bool F16 = true, OWN = true;
+    float alpha;             // of A
+    float a, b, c;           // Q = a + b A + c A^2
+    bf16_t* O; int64_t ldo;  // as OrthoApply; C: the next X (pitch ldc)
+    int K, N;                // O's
+    float scale;
+    int tall;                // X is R x S
+
+    template <typename C, int BM, int BN>
+    static __device__ __forceinline__ void finish(const OrthoStep& g, f32x4 (&acc)[C::TM][C::TN], int, int, const int wm, const int wn, const int tid, char* smem);
+};
+// An S x S matrix in LDS as KC operands are read: for each 64 columns, S rows of 128 bytes with their chunks permuted.
+template <int S>
+__device__ __forceinline__ int image_at(int row, int col) {
+    return (col >> 6) * (S * 128) + row * 128 + ((((col >> 3) & 7) ^ swz_kc(row)) << 4) + (col & 7) * 2;
+}
+template <typename C, int S, int S2>
+__device__ __forceinline__ void OrthoStep::finish(const OrthoStep& g, f32x4 (&acc)[C::TM][C::TN], int, int, const int wm, const int wn, const int tid, char* smem) {
+    static_assert(S == S2 && C::WAVES * 16 == S, "a wave to 16 rows");
+    constexpr int IMAGE = S * S * 2, SLAB_CHUNKS = S * 8 / C::THREADS;
+    static_assert(2 * IMAGE + S * 128 <= C::LDS_BYTES, "A, Q and the slab in the operand buffers");
+    char *const a_image = smem, *const q_image = smem + IMAGE, *const slab = smem + 2 * IMAGE;
+    const int lane = tid & 63, wave = tid >> 6, l0 = blockIdx.x * 64;
+    // the slab: S rows of 64 columns, or 64 rows of S; its 16-byte chunks on their way into the layout that their product reads
+    u32x4 x[SLAB_CHUNKS];
+    int x_at[SLAB_CHUNKS];
+#pragma unroll
+    for (int i = 0; i < SLAB_CHUNKS; ++i) {
+        const int q = i * C::THREADS + tid;
+        if (g.tall) {
+            const int row = q / (S / 8), chunk = q % (S / 8);
+            x[i] = *reinterpret_cast<const u32x4*>(g.A + (int64_t)(l0 + row) * g.lda + chunk * 8);
+            x_at[i] = image_at<64>(row, chunk * 8);
+        } else {
+            const int row = q / 8, chunk = q % 8;
+            x[i] = *reinterpret_cast<const u32x4*>(g.A + (int64_t)row * g.lda + l0 + chunk * 8);
+            x_at[i] = row * 128 + ((chunk ^ swz_mc<64>(row)) << 4);
+        }
+    }
+    const int r = lane & 15, c4 = 4 * (lane >> 4);
+    auto put = [&](char* image, int row, int col, f32x4 v) __attribute__((always_inline)) {
+        *reinterpret_cast<uint2*>(image + image_at<S>(row, col)) = uint2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+    };
+    __syncthreads();  // all waves are done reading the operand buffers
+#pragma unroll
+    for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+        for (int b = 0; b < C::TN; ++b) {
+            acc[a][b] = acc[a][b] * g.alpha;
+            put(a_image, wm * C::WTM + a * 16 + r, wn * C::WTN + b * 16 + c4, acc[a][b]);
+        }
+#pragma unroll
+    for (int i = 0; i < SLAB_CHUNKS; ++i) *reinterpret_cast<u32x4*>(slab + x_at[i]) = x[i];
+    __syncthreads();
+    {
+        f32x4 sum[C::TM][C::TN];
+        FragAddr<S, KC, C::TM> fa;
+        FragAddr<S, KC, C::TN> fb;
+        fa.init(wm * C::WTM, lane, 0);
+        fb.init(wn * C::WTN, lane, 0);
+#pragma unroll
+        for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+            for (int b = 0; b < C::TN; ++b) sum[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < S / 64; ++k)
+#pragma unroll
+            for (int kq = 0; kq < 2; ++kq) {
+                bf16x8 av[C::TM], bv[C::TN];
+#pragma unroll
+                for (int a = 0; a < C::TM; ++a) av[a] = fa.read(a_image, k, a, kq);
+#pragma unroll
+                for (int b = 0; b < C::TN; ++b) bv[b] = fb.read(a_image, k, b, kq);
+#pragma unroll
+                for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+                    for (int b = 0; b < C::TN; ++b) sum[a][b] = mfma_16x16x32<true>(bv[b], av[a], sum[a][b]);
+            }
+#pragma unroll
+        for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+            for (int b = 0; b < C::TN; ++b) {
+                const int row = wm * C::WTM + a * 16 + r, col = wn * C::WTN + b * 16 + c4;
+                f32x4 v = sum[a][b] * g.c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)  // A as it is held, in fp16
+                    v[e] = __builtin_fmaf(g.b, (float)(_Float16)acc[a][b][e], v[e]) + (row == col + e ? g.a : 0.f);
+                put(q_image, row, col, v);
+            }
+    }
+    __syncthreads();
+    // 16 rows of Q by the slab, or the slab by 16 columns of Q: four tiles of 16 x 16 to a wave
+    f32x4 out[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) out[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    FragAddr<S, KC, 1> fq;
+    fq.init(wave * 16, lane, 0);
+    if (g.tall) {
+        FragAddr<64, KC, 4> fx;
+        fx.init(0, lane, 0);
+#pragma unroll
+        for (int k = 0; k < S / 64; ++k)
+#pragma unroll
+            for (int kq = 0; kq < 2; ++kq) {
+                const bf16x8 q = fq.read(q_image, k, 0, kq);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) out[t] = mfma_16x16x32<true>(q, fx.read(slab, k, t, kq), out[t]);
+            }
+    } else {
+        FragAddr<64, MC, 4> fx;
+        fx.init(0, lane, 0);
+#pragma unroll
+        for (int k = 0; k < S / 64; ++k)
+#pragma unroll
+            for (int kq = 0; kq < 2; ++kq) {
+                const bf16x8 q = fq.read(q_image, k, 0, kq);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) out[t] = mfma_16x16x32<true>(fx.read(slab, k, t, kq), q, out[t]);
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int row = g.tall ? l0 + t * 16 + r : wave * 16 + r, col = g.tall ? wave * 16 + c4 : l0 + t * 16 + c4;
+        if (!g.O) {
+            *reinterpret_cast<uint2*>(g.C + (int64_t)row * g.ldc + col) = uint2{pack_f16x2(out[t][0], out[t][1]), pack_f16x2(out[t][2], out[t][3])};
+            continue;
+        }
+        GemmArgs to;
+        to.C = g.O;
+        to.ldc = g.ldo;
+        if (row < g.K && col < g.N) store_bf16_quad(to, out[t] * g.scale, row, col, min(4, g.N - col));
+    }
+}
+template <int S, int LAYOUT>
+__global__ void __launch_bounds__(S * 4, 1) ortho_step_kernel(OrthoStep g) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    if constexpr (S == 64) gemm_ring_body<64, 64, 2, 2, 4, LAYOUT, LAYOUT>(g, 0, 0, smem, threadIdx.x);
+    else gemm_ring_body<128, 128, 4, 2, 4, LAYOUT, LAYOUT>(g, 0, 0, smem, threadIdx.x);
 }
 
 // ---- apply --------------------------------------------------------------------------------------

@@ -111,6 +111,13 @@ struct SymPlan {
 // The quickest of all kinds for s rows and columns, the tiles that do not fill a round taken whole, in slices, or in slices and rests.
 inline SymPlan sym_plan(int64_t s, int64_t steps, int64_t compute_units) {
     SymPlan best;
+    {   // 32 x 32 tiles whose four waves split the reduction, five workgroups to a compute unit: bound by what a compute unit takes in, or by one wave's chain of steps
+        // (256 columns, 16 steps; 512, 8; 576, 16; 1024, 16: see SLIM_MODEL, which these times are those of)
+        const int64_t n = (s + 31) / 32, tiles = n * (n + 1) / 2, rounds = (tiles + compute_units - 1) / compute_units;
+        const double chain = 0.7 + 0.24 * (double)((steps + 3) / 4);
+        const double us = 2.5 + std::max((double)rounds * (0.2 + 0.08 * (double)steps), (double)((rounds + 4) / 5) * chain);
+        if (tiles <= 5 * compute_units) best = {32, (int)tiles, us, {(int)steps, (int)tiles, 0, 1, 0, 0, 0, 1}};
+    }
     for (const SymKind& k : SYM_KINDS) {
         const int64_t n = (s + k.size - 1) / k.size, tiles = n * (n + 1) / 2, most = compute_units * k.beside, rounds = tiles / most, left = tiles % most;
         // so many steps one behind the other, on so many workgroups
