@@ -35,48 +35,66 @@ int launch_resnorm_typed(const axo::ResnormArgs& g, hipStream_t st) {
     return launched();
 }
 
+// Whether the column sums of the backward pass come from a second pass over the data (resnorm_cols_kernel), and where that has its rows' means and its counters in the
+// workspace, behind the sums of the slices.
+bool resnorm_two_passes(int64_t K) { return K > RESNORM_MOST_COLS; }
 size_t resnorm_partial_bytes(int64_t M, int64_t K) { return (size_t)std::max<int64_t>(1, std::min<int64_t>(M, NORM_MOST_SLICES)) * 4 * (size_t)norm_partial_cols(K) * sizeof(float); }
-size_t resnorm_workspace(int64_t M, int64_t K) { return K == 0 ? 0 : resnorm_partial_bytes(M, K) + (K > RESNORM_MOST_COLS ? ((size_t)M * sizeof(float2) + 15) / 16 * 16 : 0); }
+size_t resnorm_means_bytes(int64_t M) { return ((size_t)M * sizeof(float2) + 15) / 16 * 16; }
+size_t resnorm_workspace(int64_t M, int64_t K) {
+    if (K == 0) return 0;
+    return resnorm_partial_bytes(M, K) + (resnorm_two_passes(K) ? resnorm_means_bytes(M) + ((size_t)K + 63) / 64 * sizeof(uint32_t) : 0);
+}
 
 int launch_resnorm_join(const axo::ResnormBwdArgs& g, hipStream_t st) {
     if (!g.want_cols) return AXO_OK;
     hipLaunchKernelGGL(axo::resnorm_join_kernel, dim3(at_most(tiles_in(g.K, axo::RESNORM_JOIN_COLS), NORM_MOST_BLOCKS)), dim3(axo::RESNORM_JOIN_THREADS), 0, st, g);
     return launched();
 }
+template <typename T, int LANES, int CH, int GROUPS, bool AHEAD>
+int launch_resnorm_bwd_groups(axo::ResnormBwdArgs& g, hipStream_t st) {
+    // a workgroup to every row, or pair of long ones, whose sums are much to write and read again (one and two: 200 x 4000 16.2 and 14.3 us, 256 x 4096 17.9 and 15.4; 8 x 4000 8.7 and 10.3,
+    // 300 x 512 8.9 and 10.0)
+    g.slices = (int)std::min<int64_t>(tiles_in(g.M, GROUPS * (g.K > 2048 && g.M >= 128 ? 2 : 1)), NORM_MOST_SLICES);
+    constexpr int lds = CH == axo::RESNORM_LDS_CHUNKS ? 2 * CH * LANES * 8 * (int)sizeof(float) : 0;
+    static std::atomic<uint64_t> raised{0};
+    if (lds > 0 && !raise_lds_limit(reinterpret_cast<const void*>(axo::resnorm_bwd_rows_kernel<T, LANES, CH, GROUPS, AHEAD>), lds, &raised)) return AXO_ERR_HIP;
+    hipLaunchKernelGGL((axo::resnorm_bwd_rows_kernel<T, LANES, CH, GROUPS, AHEAD>), dim3((unsigned)g.slices), dim3(LANES * GROUPS), lds, st, g);
+    return launched();
+}
 template <typename T, int LANES, int CH>
 int launch_resnorm_bwd_rows(axo::ResnormBwdArgs& g, hipStream_t st) {
-    constexpr int GROUPS = 512 / LANES;
-    g.slices = (int)std::min<int64_t>(tiles_in(g.M, GROUPS), NORM_MOST_SLICES);
-    hipLaunchKernelGGL((axo::resnorm_bwd_rows_kernel<T, LANES, CH, GROUPS>), dim3((unsigned)g.slices), dim3(LANES * GROUPS), 0, st, g);
-    if (const int rc = launched()) return rc;
-    return launch_resnorm_join(g, st);
+    // the next row's loads ahead, as long as there are registers for them
+    return launch_resnorm_bwd_groups<T, LANES, CH, CH == 1 ? 512 / LANES : 1, CH == 1 || (CH == 2 && sizeof(T) == 2)>(g, st);
 }
 template <typename T>
 int launch_resnorm_bwd_typed(axo::ResnormBwdArgs g, hipStream_t st) {
-    if (g.M > 0 && g.K <= RESNORM_MOST_COLS) {
-        if (g.K <= 64) return launch_resnorm_bwd_rows<T, 8, 1>(g, st);
-        if (g.K <= 128) return launch_resnorm_bwd_rows<T, 16, 1>(g, st);
-        if (g.K <= 256) return launch_resnorm_bwd_rows<T, 32, 1>(g, st);
-        if (g.K <= 512) return launch_resnorm_bwd_rows<T, 64, 1>(g, st);
-        if (g.K <= 1024) return launch_resnorm_bwd_rows<T, 128, 1>(g, st);
-        if (g.K <= 2048) return launch_resnorm_bwd_rows<T, 256, 1>(g, st);
-        if (g.K <= 4096) return launch_resnorm_bwd_rows<T, 512, 1>(g, st);
-        if (g.K <= 8192) return launch_resnorm_bwd_rows<T, 512, 2>(g, st);
-        if (g.K <= 12288) return launch_resnorm_bwd_rows<T, 512, 3>(g, st);
-        return launch_resnorm_bwd_rows<T, 512, 4>(g, st);
-    }
     if (g.M > 0) {
-        hipLaunchKernelGGL(axo::resnorm_bwd_long_kernel<T>, dim3(at_most(g.M, NORM_MOST_BLOCKS)), dim3(axo::NORM_THREADS), 0, st, g);
-        if (const int rc = launched()) return rc;
+        const int rc = [&] {
+            if (g.K <= 64) return launch_resnorm_bwd_rows<T, 8, 1>(g, st);
+            if (g.K <= 128) return launch_resnorm_bwd_rows<T, 16, 1>(g, st);
+            if (g.K <= 256) return launch_resnorm_bwd_rows<T, 32, 1>(g, st);
+            if (g.K <= 512) return launch_resnorm_bwd_rows<T, 64, 1>(g, st);
+            if (g.K <= 1024) return launch_resnorm_bwd_rows<T, 128, 1>(g, st);
+            if (g.K <= 2048) return launch_resnorm_bwd_rows<T, 256, 1>(g, st);
+            if (g.K <= 4096) return launch_resnorm_bwd_rows<T, 512, 1>(g, st);
+            if (g.K <= 8192) return launch_resnorm_bwd_rows<T, 512, 2>(g, st);
+            if (g.K <= 12288) return launch_resnorm_bwd_rows<T, 512, 3>(g, st);
+            if (g.K <= RESNORM_MOST_COLS) return launch_resnorm_bwd_rows<T, 512, 4>(g, st);
+            hipLaunchKernelGGL(axo::resnorm_bwd_long_kernel<T>, dim3(at_most(g.M, NORM_MOST_BLOCKS)), dim3(axo::NORM_THREADS), 0, st, g);
+            return launched();
+        }();
+        if (rc) return rc;
     }
     if (!g.want_cols) return AXO_OK;
+    if (!g.means) return launch_resnorm_join(g, st);
+    if (g.M == 0) {  // sums of nothing
+        g.slices = 0;
+        return launch_resnorm_join(g, st);
+    }
     g.rows_per_slice = norm_slice_rows(g.M);
     g.slices = (int)tiles_in(g.M, g.rows_per_slice);
-    if (g.M > 0) {
-        hipLaunchKernelGGL(axo::resnorm_cols_kernel<T>, dim3(at_most(tiles_in(g.K, axo::NORM_STRIP) * g.slices, NORM_MOST_BLOCKS)), dim3(axo::NORM_COL_THREADS), 0, st, g);
-        if (const int rc = launched()) return rc;
-    }
-    return launch_resnorm_join(g, st);
+    hipLaunchKernelGGL(axo::resnorm_cols_kernel<T>, dim3(at_most(tiles_in(g.K, axo::NORM_STRIP) * g.slices, NORM_MOST_BLOCKS)), dim3(axo::NORM_COL_THREADS), 0, st, g);
+    return launched();
 }
 
 // What both passes check: the problem, and the norms' kinds.
@@ -171,7 +189,11 @@ int axo_resnorm_bwd(const axo_problem_t* p, const void* dY, int64_t lddy, const 
         if (!aligned16(ws)) return AXO_ERR_MISALIGNED;
         g.partial = static_cast<float*>(ws);
         g.partial_cols = norm_partial_cols(s.Kl);
-        g.means = reinterpret_cast<float2*>(static_cast<char*>(ws) + resnorm_partial_bytes(s.M, s.Kl));
+        if (resnorm_two_passes(s.Kl)) {
+            char* const behind = static_cast<char*>(ws) + resnorm_partial_bytes(s.M, s.Kl);
+            g.means = reinterpret_cast<float2*>(behind);
+            g.counters = reinterpret_cast<uint32_t*>(behind + resnorm_means_bytes(s.M));
+        }
         b.writes(ws, (int64_t)need, 1, (int64_t)need, 1);
     }
     if (const int rc = b.check()) return rc;

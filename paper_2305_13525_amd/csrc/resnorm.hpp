@@ -36,7 +36,8 @@ struct ResnormBwdArgs {
     const f32x4* stats;
     float *dgamma_a, *dbeta_a, *dgate, *dgamma_b, *dbeta_b;  // any may be nullptr
     float* partial;        // [slices x 4 x partial_cols]: Y0, Y1, S0, S1 of row slices
-    float2* means;         // of rows too long for registers: (mean(g), mean(g hb))
+    float2* means;         // (mean(g), mean(g hb)) per row, or nullptr: for resnorm_cols_kernel, whose
+    uint32_t* counters;    // strips have one each
     int64_t partial_cols;  // K, up to a whole chunk
     int slices, rows_per_slice;
     int M, K, kind_a, kind_b, accumulate, want_cols;
@@ -81,11 +82,12 @@ __device__ __forceinline__ void row_moments(const float (&v)[CH][8], int K, int 
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
         const int left = K - (j * LANES + lane) * 8;
+        if (left >= 8)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = i < left ? v[j][i] - mean : 0.f;
-            sum[0] += d * d;
-        }
+            for (int i = 0; i < 8; ++i) sum[0] += (v[j][i] - mean) * (v[j][i] - mean);
+        else
+#pragma unroll
+            for (int i = 0; i < 7; ++i) sum[0] += i < left ? (v[j][i] - mean) * (v[j][i] - mean) : 0.f;
     }
     row_sums<LANES>(sum, lds[1]);
     rstd = 1.0f / sqrtf(sum[0] / (float)K + eps);
@@ -100,13 +102,23 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES) resnorm_rows_kernel
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * ROWS + row_group<LANES>(); row < g.M; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
         const bool last = row == g.M - 1;
-        RowChunks<bf16_t, LANES, CH> b, gamma, beta, gate;
+        // The vectors, the same for all rows and from the caches: along with the row, or, of long rows, for which that takes registers away from other rows, once they are wanted.
+        constexpr bool LATE = CH > 2, EARLY = CH == 1;
+        RowChunks<bf16_t, LANES, CH> b, gamma, beta, gate, gamma_b, beta_b;
         RowChunks<T, LANES, CH> x;
         b.load(g.B + row * g.ldb, g.K, lane, last);
         x.load(static_cast<const T*>(g.X) + row * g.ldx, g.K, lane, last);
-        load_vector(gamma, g.gamma_a, g.K, lane, ONES);
-        load_vector(beta, g.beta_a, g.K, lane, 0u);
-        load_vector(gate, g.gate, g.K, lane, ONES);
+        auto first_vectors = [&]() __attribute__((always_inline)) {
+            load_vector(gamma, g.gamma_a, g.K, lane, ONES);
+            load_vector(beta, g.beta_a, g.K, lane, 0u);
+            load_vector(gate, g.gate, g.K, lane, ONES);
+        };
+        auto second_vectors = [&]() __attribute__((always_inline)) {
+            load_vector(gamma_b, g.gamma_b, g.K, lane, ONES);
+            load_vector(beta_b, g.beta_b, g.K, lane, 0u);
+        };
+        if (!LATE) first_vectors();
+        if (EARLY) second_vectors();
         b.mask(g.K, lane);
         x.mask(g.K, lane);
         float v[CH][8], mean_a, rstd_a, mean_b, rstd_b;
@@ -115,26 +127,30 @@ __global__ void __launch_bounds__(LANES <= 64 ? 256 : LANES) resnorm_rows_kernel
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[j][i] = b.raw[j].at(i);
         row_moments<LANES, CH>(v, g.K, lane, g.kind_a, g.eps, lds[turn][0], mean_a, rstd_a);
+        if (LATE) first_vectors();
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = (j * LANES + lane) * 8, left = g.K - c;
             float s[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float z = (v[j][i] - mean_a) * rstd_a * gamma.raw[j].at(i) + beta.raw[j].at(i);
-                s[i] = x.raw[j].at(i) + g.scale * gate.raw[j].at(i) * z;
-                v[j][i] = i < left ? stored(s[i], static_cast<const T*>(nullptr)) : 0.f;  // the norm is that of what is stored
+                const float h = (v[j][i] - mean_a) * rstd_a;
+                s[i] = __builtin_fmaf(g.scale * gate.raw[j].at(i), __builtin_fmaf(h, gamma.raw[j].at(i), beta.raw[j].at(i)), x.raw[j].at(i));
+                v[j][i] = stored(s[i], static_cast<const T*>(nullptr));  // the norm is that of what is stored
             }
+            if (left < 8)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = i < left ? v[j][i] : 0.f;
             store_in_row<LANES>(static_cast<T*>(g.S) + row * g.lds, g.K, c, s);
         }
-        load_vector(gamma, g.gamma_b, g.K, lane, ONES);
-        load_vector(beta, g.beta_b, g.K, lane, 0u);
+        if (!EARLY && !LATE) second_vectors();
         row_moments<LANES, CH>(v, g.K, lane, g.kind_b, g.eps, lds[turn][1], mean_b, rstd_b);
+        if (LATE) second_vectors();
         if (lane == 0 && g.stats) g.stats[row] = f32x4{mean_a, rstd_a, mean_b, rstd_b};
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[j][i] = (v[j][i] - mean_b) * rstd_b * gamma.raw[j].at(i) + beta.raw[j].at(i);
+            for (int i = 0; i < 8; ++i) v[j][i] = __builtin_fmaf((v[j][i] - mean_b) * rstd_b, gamma_b.raw[j].at(i), beta_b.raw[j].at(i));
             store_in_row<LANES>(g.Y + row * g.ldy, g.K, (j * LANES + lane) * 8, v[j]);
         }
     }
@@ -194,27 +210,43 @@ __global__ void __launch_bounds__(NORM_THREADS) resnorm_long_kernel(ResnormArgs 
     }
 }
 
+// The counters of a launch of resnorm_cols_kernel behind this one.
+__device__ __forceinline__ void resnorm_clear_counters(const ResnormBwdArgs& g) {
+    if (!g.means) return;
+    const int strips = (g.K + NORM_STRIP - 1) / NORM_STRIP;
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < strips; i += gridDim.x * blockDim.x) g.counters[i] = 0u;
+}
+
 // Backward on rows in registers, one pass over the data: a workgroup of GROUPS rows at a time walks the rows, every lane keeps the four sums of its columns as it goes.
 // At its end a workgroup adds its groups' columns up through LDS, in order, and writes them to `partial`, which resnorm_join_kernel adds up: no atomics, the same bits
 // every time.
-template <typename T, int LANES, int CH, int GROUPS>
+// AHEAD: the next row's loads are under way while this one's sums meet.
+constexpr int RESNORM_LDS_CHUNKS = 4;
+template <typename T, int LANES, int CH, int GROUPS, bool AHEAD>
 __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(ResnormBwdArgs g) {
     constexpr int BLOCK = LANES * GROUPS;
-    // registers for the next row's loads while this one's sums meet
-    constexpr bool AHEAD = CH == 1 || (CH == 2 && sizeof(T) == 2);
     __shared__ float lds[2][2][2 * (BLOCK / 64)];
     __shared__ __attribute__((aligned(16))) float cols[GROUPS > 1 ? BLOCK * 8 : 4];
     const int lane = threadIdx.x % LANES, group = row_group<LANES>();
     const float per_row = 1.0f / (float)g.K;
-    float y0[CH][8], y1[CH][8], s0[CH][8], s1[CH][8];
+    // four chunks of four sums each are half of a thread's registers: two of the sums are kept in LDS then, where a lane has places of its own
+    constexpr bool IN_LDS = CH == RESNORM_LDS_CHUNKS;
+    constexpr int IN_REGS = IN_LDS ? 1 : CH;
+    extern __shared__ __attribute__((aligned(16))) float y_sums[];
+    auto y_at = [&](int what, int j, int half) __attribute__((always_inline)) { return reinterpret_cast<f32x4*>(y_sums) + ((what * CH + j) * 2 + half) * LANES + lane; };
+    float y0[IN_REGS][8], y1[IN_REGS][8], s0[CH][8], s1[CH][8];
 #pragma unroll
     for (int j = 0; j < CH; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y0[j][i] = y1[j][i] = s0[j][i] = s1[j][i] = 0.f;
+        for (int i = 0; i < 8; ++i) {
+            y0[j % IN_REGS][i] = y1[j % IN_REGS][i] = s0[j][i] = s1[j][i] = 0.f;
+            if (IN_LDS && i < 4) *y_at(i / 2, j, i % 2) = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     RowChunks<bf16_t, LANES, CH> gb, ga, gate;
     load_vector(gb, g.gamma_b, g.K, lane, ONES);
     load_vector(ga, g.gamma_a, g.K, lane, ONES);
     load_vector(gate, g.gate, g.K, lane, ONES);
+    resnorm_clear_counters(g);
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     RowChunks<T, LANES, CH> s_next, ds_next;
     RowChunks<bf16_t, LANES, CH> dy_next, b_next;
@@ -256,19 +288,33 @@ __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(Resnor
         }
         float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
+        for (int j = 0; j < CH; ++j) {
+            f32x4 held[4];  // of this chunk: y0's two quads, y1's
+            if constexpr (IN_LDS)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) held[q] = *y_at(q / 2, j, q % 2);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float y = dy.raw[j].at(i), h = hb_of(j, i), d = y * gb.raw[j].at(i);
-                y0[j][i] += y * h;
-                y1[j][i] += y;
-                asm volatile("" : "+v"(y0[j][i]), "+v"(y1[j][i]));  // here: put off, they would keep h and y in registers
+                if constexpr (IN_LDS) {
+                    held[i / 4][i % 4] += y * h;
+                    held[2 + i / 4][i % 4] += y;
+                } else {
+                    y0[j][i] += y * h;
+                    y1[j][i] += y;
+                    asm volatile("" : "+v"(y0[j][i]), "+v"(y1[j][i]));  // here: put off, they would keep h and y in registers
+                }
                 sum[0] += d;
                 sum[1] += d * h;
             }
+            if constexpr (IN_LDS)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) *y_at(q / 2, j, q % 2) = held[q];
+        }
         if (AHEAD && row0 + step < g.M) request(row + step);
         row_sums<LANES>(sum, lds[turn][0]);
         const float c1 = g.kind_b == KIND_LAYER ? sum[0] * per_row : 0.f, c2 = sum[1] * per_row;
+        if (g.means && here && lane == 0) g.means[row] = float2{c1, c2};
         float d[CH][8];  // ds'
         sum[0] = sum[1] = 0.f;
 #pragma unroll
@@ -278,13 +324,16 @@ __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(Resnor
             const int left = here ? g.K - (j * LANES + lane) * 8 : 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float v = ds.raw[j].at(i) + st[3] * (dy.raw[j].at(i) * gb.raw[j].at(i) - c1 - hb_of(j, i) * c2);
-                d[j][i] = i < left ? v : 0.f;
+                d[j][i] = ds.raw[j].at(i) + st[3] * (dy.raw[j].at(i) * gb.raw[j].at(i) - c1 - hb_of(j, i) * c2);
+            }
+            if (left < 8)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[j][i] = i < left ? d[j][i] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
                 const float h = ha_of(j, i), q = g.scale * gate.raw[j].at(i) * ga.raw[j].at(i) * d[j][i];
-                if (here) {
-                    s0[j][i] += d[j][i] * h;
-                    s1[j][i] += d[j][i];
-                }
+                s0[j][i] += d[j][i] * h;  // zeros, of a row that is not there
+                s1[j][i] += d[j][i];
                 asm volatile("" : "+v"(s0[j][i]), "+v"(s1[j][i]));
                 sum[0] += q;
                 sum[1] += q * h;
@@ -306,24 +355,31 @@ __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(Resnor
             store_in_row<LANES>(g.dB + row * g.lddb, g.K, (j * LANES + lane) * 8, d[j]);
         }
     }
-    if (!g.want_cols) return;
+    if (!g.want_cols || g.means) return;
     constexpr int COLS = LANES * 8;  // of a chunk of all lanes
 #pragma unroll
     for (int what = 0; what < 4; ++what) {
-        const float(&v)[CH][8] = what == 0 ? y0 : what == 1 ? y1 : what == 2 ? s0 : s1;
+        float v[CH][8];
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[j][i] = what == 2 ? s0[j][i] : what == 3 ? s1[j][i] : IN_LDS ? (*y_at(what, j, i / 4))[i % 4] : what == 0 ? y0[j % IN_REGS][i] : y1[j % IN_REGS][i];
         float* const to = g.partial + ((int64_t)blockIdx.x * 4 + what) * g.partial_cols;
         if constexpr (GROUPS > 1) {
-            static_assert(CH == 1, "a chunk per lane");
-            __syncthreads();
-            float* const mine = cols + group * COLS + lane * 8;
-            *reinterpret_cast<f32x4*>(mine) = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
-            *reinterpret_cast<f32x4*>(mine + 4) = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
-            __syncthreads();
-            for (int c = threadIdx.x; c < COLS && c < g.K; c += BLOCK) {
-                float sum = 0.f;
 #pragma unroll
-                for (int q = 0; q < GROUPS; ++q) sum += cols[q * COLS + c];
-                to[c] = sum;
+            for (int j = 0; j < CH; ++j) {
+                __syncthreads();
+                float* const mine = cols + group * COLS + lane * 8;
+                *reinterpret_cast<f32x4*>(mine) = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
+                *reinterpret_cast<f32x4*>(mine + 4) = f32x4{v[j][4], v[j][5], v[j][6], v[j][7]};
+                __syncthreads();
+                for (int c = threadIdx.x; c < COLS && j * COLS + c < g.K; c += BLOCK) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int q = 0; q < GROUPS; ++q) sum += cols[q * COLS + c];
+                    to[j * COLS + c] = sum;
+                }
             }
         } else {
 #pragma unroll
@@ -360,6 +416,7 @@ template <typename T>
 __global__ void __launch_bounds__(NORM_THREADS) resnorm_bwd_long_kernel(ResnormBwdArgs g) {
     __shared__ float lds[2 * NORM_THREADS / 64];
     const float per_row = 1.0f / (float)g.K;
+    resnorm_clear_counters(g);
     for (int64_t row = blockIdx.x; row < g.M; row += gridDim.x) {
         const f32x4 st = g.stats[row];
         float sum[2] = {0.f, 0.f};
@@ -378,7 +435,7 @@ __global__ void __launch_bounds__(NORM_THREADS) resnorm_bwd_long_kernel(ResnormB
         }
         block_sums<NORM_THREADS>(sum, lds);
         const float2 m = {g.kind_b == KIND_LAYER ? sum[0] * per_row : 0.f, sum[1] * per_row};
-        if (threadIdx.x == 0 && g.want_cols) g.means[row] = m;
+        if (threadIdx.x == 0 && g.means) g.means[row] = m;
         // q and ha of a chunk
         auto chunk = [&](int64_t c, int valid, float (&d)[8], float (&q)[8], float (&ha)[8]) __attribute__((always_inline)) {
             float w[8];
@@ -418,10 +475,28 @@ __global__ void __launch_bounds__(NORM_THREADS) resnorm_bwd_long_kernel(ResnormB
     }
 }
 
-// The four column sums of such rows: strips of 64 columns over slices of the rows, 8 lanes of 8 columns by 32 rows at a time, as norm_cols_kernel.
+// The gradients of column c from its four sums.
+__device__ __forceinline__ void resnorm_gradients(const ResnormBwdArgs& g, int64_t c, const float (&v)[4]) {
+    const float gate = g.scale * (g.gate ? bf16_bits_to_f32(g.gate[c]) : 1.f);
+    const float gamma = g.gamma_a ? bf16_bits_to_f32(g.gamma_a[c]) : 1.f, beta = g.beta_a ? bf16_bits_to_f32(g.beta_a[c]) : 0.f;
+    auto out = [&](float* to, float x) __attribute__((always_inline)) {
+        if (to) to[c] = g.accumulate ? to[c] + x : x;
+    };
+    out(g.dgamma_b, v[0]);
+    out(g.dbeta_b, v[1]);
+    out(g.dgamma_a, gate * v[2]);
+    out(g.dbeta_a, gate * v[3]);
+    out(g.dgate, g.scale * (gamma * v[2] + beta * v[3]));
+}
+
+// The four column sums of rows whose dX and dB have been formed, and the gradients: strips of 64 columns over slices of the rows, 8 lanes of 8 columns by 32 rows at a
+// time, as norm_cols_kernel.  A slice's sums go to the workspace, and whoever comes last of a strip adds them up in the slices' order (as the slices of gated_slim_kernel:
+// past the L2, by device-scope accesses).
+// It reads the data a second time, and is for few rows: those come from the caches, and 256 slices of sums, as a pass over rows in registers leaves them, would be as much.
 template <typename T>
 __global__ void __launch_bounds__(NORM_COL_THREADS) resnorm_cols_kernel(ResnormBwdArgs g) {
     __shared__ float lds[4][NORM_COL_THREADS / 64][NORM_STRIP];
+    __shared__ uint32_t arrived;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t pieces = ((int64_t)g.K + NORM_STRIP - 1) / NORM_STRIP * g.slices;
     for (int64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
@@ -467,28 +542,50 @@ __global__ void __launch_bounds__(NORM_COL_THREADS) resnorm_cols_kernel(ResnormB
 #pragma unroll
         for (int w = 0; w < NORM_COL_THREADS / 64; ++w) all += lds[what][w][c];
         const int64_t at = strip * NORM_STRIP + c;
-        if (at < g.K) g.partial[(slice * 4 + what) * g.partial_cols + at] = all;
+        if (at < g.K) __hip_atomic_store(g.partial + (slice * 4 + what) * g.partial_cols + at, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's sums have arrived where all XCDs see them
+        __syncthreads();                                  // and those of all waves; lds has been read
+        if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(g.counters + strip, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (arrived != (uint32_t)(g.slices - 1)) continue;
+        all = 0.f;
+        if (at < g.K)
+            for (int s0 = 0; s0 < g.slices; s0 += 8) {  // eight slices requested at a time
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[i] = s0 + i < g.slices ? __hip_atomic_load(g.partial + ((int64_t)(s0 + i) * 4 + what) * g.partial_cols + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) all += v[i];
+            }
+        lds[what][0][c] = all;
+        __syncthreads();
+        if (what == 0 && at < g.K) {
+            const float v[4] = {all, lds[1][0][c], lds[2][0][c], lds[3][0][c]};
+            resnorm_gradients(g, at, v);
+        }
     }
 }
 
-// The sums of all slices, added in an order that depends on their number alone, and what is formed of them.  A workgroup has 32 columns: 256 threads to each of the four
-// sums, eight lanes of 16 bytes by every 32nd slice; the lanes of a wave meet by exchanges and the waves in LDS.
+// The sums of all slices, added in an order that depends on their number and the columns' alone, and what is formed of them.  A workgroup has 32 columns: 256 threads to each of
+// the four sums, eight lanes of 16 bytes by every 32nd slice; the lanes of a wave meet by exchanges and the waves in LDS.  (Eight columns, 32 bytes of a slice's line: 200 x 4000 20.5 us as a
+// whole, now 14.3.)
 constexpr int RESNORM_JOIN_THREADS = 1024, RESNORM_JOIN_COLS = 32;
 __global__ void __launch_bounds__(RESNORM_JOIN_THREADS) resnorm_join_kernel(ResnormBwdArgs g) {
-    constexpr int WAVES = RESNORM_JOIN_THREADS / 64 / 4;  // of a sum
+    constexpr int WAVES = RESNORM_JOIN_THREADS / 64 / 4, LANES = RESNORM_JOIN_COLS / 4;  // of a sum; that share a slice
     __shared__ __attribute__((aligned(16))) float lds[4][WAVES][RESNORM_JOIN_COLS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, what = wave / WAVES;
     for (int64_t from = (int64_t)blockIdx.x * RESNORM_JOIN_COLS; from < g.K; from += (int64_t)gridDim.x * RESNORM_JOIN_COLS) {
-        const int64_t col = from + (lane & 7) * 4;
+        const int64_t col = from + lane % LANES * 4;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         if (col < g.partial_cols)
-            for (int s = (threadIdx.x & 255) >> 3; s < g.slices; s += 32) sum += *reinterpret_cast<const f32x4*>(g.partial + ((int64_t)s * 4 + what) * g.partial_cols + col);
+            for (int s = (threadIdx.x & 255) / LANES; s < g.slices; s += 256 / LANES) sum += *reinterpret_cast<const f32x4*>(g.partial + ((int64_t)s * 4 + what) * g.partial_cols + col);
 #pragma unroll
-        for (int m = 8; m < 64; m <<= 1)
+        for (int m = LANES; m < 64; m <<= 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m, 64);
         __syncthreads();  // the last columns' sums have been read
-        if (lane < 8) *reinterpret_cast<f32x4*>(&lds[what][wave % WAVES][lane * 4]) = sum;
+        if (lane < LANES) *reinterpret_cast<f32x4*>(&lds[what][wave % WAVES][lane * 4]) = sum;
         __syncthreads();
         const int64_t c = from + threadIdx.x;
         if (threadIdx.x >= RESNORM_JOIN_COLS || c >= g.K) continue;
@@ -499,16 +596,7 @@ __global__ void __launch_bounds__(RESNORM_JOIN_THREADS) resnorm_join_kernel(Resn
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) v[w] += lds[w][i][threadIdx.x];
         }
-        const float gate = g.scale * (g.gate ? bf16_bits_to_f32(g.gate[c]) : 1.f);
-        const float gamma = g.gamma_a ? bf16_bits_to_f32(g.gamma_a[c]) : 1.f, beta = g.beta_a ? bf16_bits_to_f32(g.beta_a[c]) : 0.f;
-        auto out = [&](float* to, float x) __attribute__((always_inline)) {
-            if (to) to[c] = g.accumulate ? to[c] + x : x;
-        };
-        out(g.dgamma_b, v[0]);
-        out(g.dbeta_b, v[1]);
-        out(g.dgamma_a, gate * v[2]);
-        out(g.dbeta_a, gate * v[3]);
-        out(g.dgate, g.scale * (gamma * v[2] + beta * v[3]));
+        resnorm_gradients(g, c, v);
     }
 }
 
