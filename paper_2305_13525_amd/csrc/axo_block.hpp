@@ -338,7 +338,8 @@ constexpr int64_t GATED_MOST_TILES = GATED_COUNTER_BYTES / sizeof(uint32_t);
 //   - one wave's chain of chunks, `latency` each, as many under way as it has stages;
 //   - the weights, read at `tbs` TB/s;
 // and `join` where its reduction is sliced.  Fitted to 14 000 shapes (1 to 800 tokens, widths of 32 to 16384, weights from memory) and for the kind that is left to
-// few rows and much weight to 1400 of those; half of the estimates are within 5 to 11 %, nine of ten within 28 %.
+// few rows and much weight to 1400 of those; half of the estimates are within 5 to 11 %, nine of ten within 28 %.  Those of the product with a residual to 20 000 (1 to 400 tokens,
+// widths of 64 to 16384), each counted by its time: 6 to 8 % and 18 to 21 %.
 struct GatedSlim {
     int rows, cols, waves, stages;  // `cols`: of the output
     double fixed, rate, alone, latency, tbs, join, each;
@@ -349,12 +350,13 @@ constexpr GatedSlim GATED_SLIM[5][4] = {
     {{16, 32, 4, 3, 4.32, 87.9, 126.6, 0.88, 6.72, 1.20, 0.66}, {32, 32, 4, 3, 3.01, 73.9, 155.4, 1.44, 5.48, 2.59, 1.84}, {}, {}},
     {{16, 32, 4, 3, 4.16, 71.8, 78.6, 1.04, 5.69, 0.71, 0.28}, {32, 32, 4, 3, 3.16, 87.1, 115.1, 1.50, 4.63, 2.34, 1.24}, {}, {}},
     {},
-    {{16, 32, 4, 3, 3.26, 39.4, 67.2, 2.37, 3.78, 2.31, 1.21}, {32, 32, 4, 3, 2.85, 42.6, 64.6, 2.99, 3.14, 3.92, 1.53},
-     {16, 64, 2, 4, 3.10, 51.8, 97.2, 2.65, 4.87, 3.79, 2.04}, {16, 128, 2, 2, 4.73, 49.3, 50.0, 3.14, 6.18, 4.74, 0.30}}};
+    {{16, 32, 4, 3, 3.20, 46.1, 67.4, 1.47, 4.14, 1.89, 0.62}, {32, 32, 4, 3, 2.03, 50.2, 82.1, 2.28, 3.84, 2.47, 1.96},
+     {16, 64, 4, 3, 2.27, 48.8, 87.5, 2.37, 4.95, 2.63, 1.75}, {16, 128, 4, 2, 4.36, 80.0, 89.9, 0.79, 5.91, 2.92, 0.00}}};
 // Rows of 256 bytes of either weight (the fourth kind) are for tokens of one tile that read more than the caches hold: there they are the quickest, 1.2 times quicker than 64 x 128
 // tiles (1 x 8192 x 16384 97 us, with rows of 128 bytes 109, on those tiles 104; where rows lie a multiple of 4 KiB apart, a column of 128 bytes
-// lies in half of each of its DRAM pages).  With less to read they are not.
-constexpr double GATED_WIDE_MB = 200.0;
+// lies in half of each of its DRAM pages).  With less to read they are not.  The product with a residual has one weight and four waves to these tiles: of 1500 shapes up to 16 tokens they
+// are the quickest kind from 100 MB on (120 to 140 MB: 1.02 times the best of all, rows of 128 bytes 1.07, 64 x 64 tiles 1.27; 60 to 80 MB 1.10 and 1.02).
+constexpr double GATED_WIDE_MB[5] = {200.0, 200.0, 200.0, 200.0, 100.0};
 // The same for the tiles of gemm_tile.hpp: what their estimates have to be multiplied with for these products (small, wide, tall, mid, big; medians of the same
 // shapes), which read weights from memory and have longer epilogues.  Whatever is estimated quicker is taken: over those shapes the choice is 1.29 (forward), 1.63 and 1.99 times
 // quicker than these tiles throughout, 3 to 5 % slower than the best of all, and by more than 5 % slower than these tiles for two or three shapes in a hundred.
@@ -384,7 +386,7 @@ GatedCut gated_cut(int Mo, int No, int R, double* us) {
     *us = 1e30;
     for (int k = 0; k < 4; ++k) {
         const GatedSlim& m = GATED_SLIM[OP][k];
-        if (m.rows == 0 || (m.rows == 16 && Mo > 256) || (k == 3 && (Mo > 16 || weights < GATED_WIDE_MB))) continue;
+        if (m.rows == 0 || (m.rows == 16 && Mo > 256) || (k == 3 && (Mo > 16 || weights < GATED_WIDE_MB[OP]))) continue;
         const int64_t tm = tiles_in(Mo, m.rows), tn = tiles_in(No, m.cols), tiles = tm * tn;
         if (tiles > 4000) continue;
         const int cols = m.cols * (OP == axo::GATED_FWD ? 2 : 1);
