@@ -210,13 +210,6 @@ __global__ void __launch_bounds__(NORM_THREADS) resnorm_long_kernel(ResnormArgs 
     }
 }
 
-// The counters of a launch of resnorm_cols_kernel behind this one.
-__device__ __forceinline__ void resnorm_clear_counters(const ResnormBwdArgs& g) {
-    if (!g.means) return;
-    const int strips = (g.K + NORM_STRIP - 1) / NORM_STRIP;
-    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < strips; i += gridDim.x * blockDim.x) g.counters[i] = 0u;
-}
-
 // Backward on rows in registers, one pass over the data: a workgroup of GROUPS rows at a time walks the rows, every lane keeps the four sums of its columns as it goes.
 // At its end a workgroup adds its groups' columns up through LDS, in order, and writes them to `partial`, which resnorm_join_kernel adds up: no atomics, the same bits
 // every time.
@@ -246,7 +239,6 @@ __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(Resnor
     load_vector(gb, g.gamma_b, g.K, lane, ONES);
     load_vector(ga, g.gamma_a, g.K, lane, ONES);
     load_vector(gate, g.gate, g.K, lane, ONES);
-    resnorm_clear_counters(g);
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     RowChunks<T, LANES, CH> s_next, ds_next;
     RowChunks<bf16_t, LANES, CH> dy_next, b_next;
@@ -314,7 +306,6 @@ __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(Resnor
         if (AHEAD && row0 + step < g.M) request(row + step);
         row_sums<LANES>(sum, lds[turn][0]);
         const float c1 = g.kind_b == KIND_LAYER ? sum[0] * per_row : 0.f, c2 = sum[1] * per_row;
-        if (g.means && here && lane == 0) g.means[row] = float2{c1, c2};
         float d[CH][8];  // ds'
         sum[0] = sum[1] = 0.f;
 #pragma unroll
@@ -355,7 +346,7 @@ __global__ void __launch_bounds__(LANES * GROUPS) resnorm_bwd_rows_kernel(Resnor
             store_in_row<LANES>(g.dB + row * g.lddb, g.K, (j * LANES + lane) * 8, d[j]);
         }
     }
-    if (!g.want_cols || g.means) return;
+    if (!g.want_cols) return;
     constexpr int COLS = LANES * 8;  // of a chunk of all lanes
 #pragma unroll
     for (int what = 0; what < 4; ++what) {
@@ -416,7 +407,10 @@ template <typename T>
 __global__ void __launch_bounds__(NORM_THREADS) resnorm_bwd_long_kernel(ResnormBwdArgs g) {
     __shared__ float lds[2 * NORM_THREADS / 64];
     const float per_row = 1.0f / (float)g.K;
-    resnorm_clear_counters(g);
+    if (g.means) {  // the counters of the resnorm_cols_kernel behind this one
+        const int strips = (g.K + NORM_STRIP - 1) / NORM_STRIP;
+        for (int i = blockIdx.x * NORM_THREADS + threadIdx.x; i < strips; i += gridDim.x * NORM_THREADS) g.counters[i] = 0u;
+    }
     for (int64_t row = blockIdx.x; row < g.M; row += gridDim.x) {
         const f32x4 st = g.stats[row];
         float sum[2] = {0.f, 0.f};
@@ -492,7 +486,7 @@ __device__ __forceinline__ void resnorm_gradients(const ResnormBwdArgs& g, int64
 // The four column sums of rows whose dX and dB have been formed, and the gradients: strips of 64 columns over slices of the rows, 8 lanes of 8 columns by 32 rows at a
 // time, as norm_cols_kernel.  A slice's sums go to the workspace, and whoever comes last of a strip adds them up in the slices' order (as the slices of gated_slim_kernel:
 // past the L2, by device-scope accesses).
-// It reads the data a second time, and is for few rows: those come from the caches, and 256 slices of sums, as a pass over rows in registers leaves them, would be as much.
+// It reads the data a second time: for rows that are too long for registers.
 template <typename T>
 __global__ void __launch_bounds__(NORM_COL_THREADS) resnorm_cols_kernel(ResnormBwdArgs g) {
     __shared__ float lds[4][NORM_COL_THREADS / 64][NORM_STRIP];
