@@ -42,8 +42,8 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
         at += (bytes + 255) / 256 * 256;
         return from;
     };
-    auto partials = [](const axo::SymPlan& y) { return (size_t)y.cut.slots() * y.size * y.size * sizeof(float); };
-    p->counters = take((size_t)std::max(p->gram.cut.cut, p->poly.cut.cut) * sizeof(uint32_t));
+    auto partials = [](const axo::SymPlan& y) { return (size_t)y.partial_floats() * sizeof(float); };
+    p->counters = take((size_t)std::max(p->gram.counters(), p->poly.counters()) * sizeof(uint32_t));
     p->sums = take(axo::ORTHO_SUMS * sizeof(double));
     p->A = take((size_t)(p->s * p->s) * 2);
     p->Q = take((size_t)(p->s * p->s) * 2);
@@ -53,13 +53,20 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
     return AXO_OK;
 }
 
+// 256 x 128 tiles, and 128 x 128 ones behind them.
+struct SymHalfCfg {
+    static constexpr int THREADS = axo::TILE_THREADS, LDS_BYTES = std::max(axo::MixSmallCfg::LDS_BYTES, axo::MidCfg::LDS_BYTES);
+    static_assert(axo::MixSmallCfg::THREADS == THREADS && axo::MidCfg::THREADS == THREADS, "one launch");
+};
 template <int SIZE, int LAYOUT>
 int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
-    using C = std::conditional_t<SIZE == 32, axo::SlimCfg<32, 32, axo::SLIM_WAVES, 1>, std::conditional_t<SIZE == 64, axo::SmallCfg<false>, std::conditional_t<SIZE == 128, axo::MidCfg, axo::MixBigCfg>>>;
+    using C = std::conditional_t<SIZE == 32, axo::SlimCfg<32, 32, axo::SLIM_WAVES, 1>, std::conditional_t<SIZE == 64, axo::SmallCfg<false>,
+        std::conditional_t<SIZE == 128, axo::MidCfg, std::conditional_t<SIZE == axo::SYM_HALF, SymHalfCfg, axo::MixBigCfg>>>>;
     auto kern = [] {
         if constexpr (SIZE == 32) return axo::ortho_sym_32_kernel<LAYOUT>;
         else if constexpr (SIZE == 64) return axo::ortho_sym_64_kernel<LAYOUT>;
         else if constexpr (SIZE == 128) return axo::ortho_sym_128_kernel<LAYOUT>;
+        else if constexpr (SIZE == axo::SYM_HALF) return axo::ortho_sym_half_kernel<LAYOUT>;
         else return axo::ortho_sym_256_kernel<LAYOUT>;
     }();
     static std::atomic<uint64_t> raised{0};
@@ -69,8 +76,10 @@ int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
 }
 int launch_sym(axo::OrthoSym g, const axo::SymPlan& y, bool tall, hipStream_t st) {
     g.cut = y.cut;
+    g.diagonal = y.diagonal;
     if (y.size == 32) return tall ? launch_sym<32, axo::MC>(g, y.workgroups, st) : launch_sym<32, axo::KC>(g, y.workgroups, st);
     if (y.size == 64) return tall ? launch_sym<64, axo::MC>(g, y.workgroups, st) : launch_sym<64, axo::KC>(g, y.workgroups, st);
+    if (y.size == axo::SYM_HALF) return tall ? launch_sym<axo::SYM_HALF, axo::MC>(g, y.workgroups, st) : launch_sym<axo::SYM_HALF, axo::KC>(g, y.workgroups, st);
     if (y.size == 128) return tall ? launch_sym<128, axo::MC>(g, y.workgroups, st) : launch_sym<128, axo::KC>(g, y.workgroups, st);
     return tall ? launch_sym<256, axo::MC>(g, y.workgroups, st) : launch_sym<256, axo::KC>(g, y.workgroups, st);
 }
@@ -110,7 +119,7 @@ int launch_load(const axo::OrthoLoadArgs& g, hipStream_t st) {
     hipLaunchKernelGGL(axo::ortho_norm_kernel<T>, dim3(axo::ORTHO_SUMS), dim3(axo::ORTHO_THREADS), 0, st, g);
     if (const int rc = launched()) return rc;
     const int64_t chunks = (int64_t)g.rows * g.cols / 8;
-    hipLaunchKernelGGL(axo::ortho_load_kernel<T>, dim3((unsigned)std::min<int64_t>(2048, (chunks + axo::ORTHO_THREADS - 1) / axo::ORTHO_THREADS)), dim3(axo::ORTHO_THREADS), 0, st, g);
+    hipLaunchKernelGGL(axo::ortho_load_kernel<T>, dim3((unsigned)std::min<int64_t>(512, (chunks + axo::ORTHO_THREADS - 1) / axo::ORTHO_THREADS)), dim3(axo::ORTHO_THREADS), 0, st, g);
     return launched();
 }
 

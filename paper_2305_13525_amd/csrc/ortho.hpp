@@ -43,18 +43,48 @@ __device__ __forceinline__ double ortho_block_sum(double v, double* lds) {
     for (int w = 0; w < ORTHO_THREADS / 64; ++w) sum += lds[w];
     return sum;
 }
+// ORTHO_AT_ONCE chunks of eight values, `step` chunks of `per_row` to a row apart: whole ones requested together, zeros outside of G.
+constexpr int ORTHO_AT_ONCE = 4;
+template <typename T>
+__device__ __forceinline__ void ortho_chunks(const OrthoLoadArgs& g, uint32_t at0, uint32_t step, uint32_t chunks, uint32_t per_row, float (&v)[ORTHO_AT_ONCE][8]) {
+    constexpr int WORDS = sizeof(T) / 2;
+    u32x4 raw[ORTHO_AT_ONCE][WORDS];
+    int valid[ORTHO_AT_ONCE];
+    const T* from[ORTHO_AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < ORTHO_AT_ONCE; ++j) {
+        const uint32_t at = at0 + j * step, row = at / per_row, col = (at - row * per_row) * 8;
+        valid[j] = at < chunks && (int)row < g.K ? min(8, g.N - (int)col) : 0;
+        from[j] = static_cast<const T*>(g.G) + (int64_t)row * g.ldg + col;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            raw[j][w] = u32x4{0u, 0u, 0u, 0u};
+            if (valid[j] == 8) raw[j][w] = reinterpret_cast<const u32x4*>(from[j])[w];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < ORTHO_AT_ONCE; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t word = WORDS == 1 ? raw[j][0][i / 2] : raw[j][i / 4 % WORDS][i % 4];
+            v[j][i] = WORDS == 1 ? bf16_bits_to_f32((bf16_t)(word >> (i % 2 * 16))) : __builtin_bit_cast(float, word);
+        }
+        if (valid[j] > 0 && valid[j] < 8) load_chunk(from[j], valid[j], v[j]);
+    }
+}
 template <typename T>
 __global__ void __launch_bounds__(ORTHO_THREADS) ortho_norm_kernel(OrthoLoadArgs g) {
     __shared__ double lds[ORTHO_THREADS / 64];
     // (fewer than 2^28 chunks, of weights of fewer than 2^31 values)
     const uint32_t per_row = ((uint32_t)g.N + 7) / 8, chunks = per_row * (uint32_t)g.K, step = gridDim.x * ORTHO_THREADS;
     double sum = 0.0;
-    for (uint32_t at = blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += step) {
-        const uint32_t row = at / per_row, col = (at - row * per_row) * 8;
-        float v[8];
-        load_chunk(static_cast<const T*>(g.G) + (int64_t)row * g.ldg + col, min(8, g.N - (int)col), v);
+    for (uint32_t at = blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += ORTHO_AT_ONCE * step) {
+        float v[ORTHO_AT_ONCE][8];
+        ortho_chunks<T>(g, at, step, chunks, per_row, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += (double)v[i] * (double)v[i];
+        for (int j = 0; j < ORTHO_AT_ONCE; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (double)v[j][i] * (double)v[j][i];
     }
     sum = ortho_block_sum(sum, lds);
     if (threadIdx.x == 0) g.sums[blockIdx.x] = sum;
@@ -65,22 +95,27 @@ __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
     return __builtin_bit_cast(uint32_t, v);
 }
 // X = G scale / (|G| + eps), zeros around it.  A gradient of zeros stays one.
+// (Products in fp64 and their conversions bound it: 2048 x 6144 27 us and 10, 4096 x 16384 88 and 46.)
 template <typename T>
 __global__ void __launch_bounds__(ORTHO_THREADS) ortho_load_kernel(OrthoLoadArgs g) {
     __shared__ double lds[ORTHO_THREADS / 64];
-    const double norm = sqrt(ortho_block_sum(threadIdx.x < ORTHO_SUMS ? g.sums[threadIdx.x] : 0.0, lds)) + (double)g.eps;
-    const double factor = norm == 0.0 ? 0.0 : g.scale / norm;
+    const double mine = threadIdx.x < ORTHO_SUMS ? g.sums[threadIdx.x] : 0.0;
     const uint32_t per_row = (uint32_t)g.cols / 8, chunks = per_row * (uint32_t)g.rows, step = gridDim.x * ORTHO_THREADS;
-    for (uint32_t at = blockIdx.x * ORTHO_THREADS + threadIdx.x; at < chunks; at += step) {
-        const uint32_t row = at / per_row, col = (at - row * per_row) * 8;
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if ((int)row < g.K && (int)col < g.N) {
-            float v[8];
-            load_chunk(static_cast<const T*>(g.G) + (int64_t)row * g.ldg + col, min(8, g.N - (int)col), v);
+    const double norm = sqrt(ortho_block_sum(mine, lds)) + (double)g.eps;
+    // scale / norm as a power of two and a number from 1/2 to 1, in that order: no product leaves the range of fp32 that X's does not leave
+    int exponent;
+    const float factor = (float)frexp(norm == 0.0 ? 0.0 : g.scale / norm, &exponent);
+    for (uint32_t at0 = blockIdx.x * ORTHO_THREADS + threadIdx.x; at0 < chunks; at0 += ORTHO_AT_ONCE * step) {
+        float v[ORTHO_AT_ONCE][8];
+        ortho_chunks<T>(g, at0, step, chunks, per_row, v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = pack_f16x2((float)((double)v[2 * i] * factor), (float)((double)v[2 * i + 1] * factor));
+        for (int j = 0; j < ORTHO_AT_ONCE; ++j) {
+            const uint32_t at = at0 + j * step;
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(ldexpf(v[j][2 * i], exponent) * factor, ldexpf(v[j][2 * i + 1], exponent) * factor);
+            if (at < chunks) *reinterpret_cast<u32x4*>(g.X + (int64_t)at * 8) = w;
         }
-        *reinterpret_cast<u32x4*>(g.X + (int64_t)at * 8) = w;
     }
 }
 
@@ -95,7 +130,7 @@ struct OrthoSym : GemmArgs {
     float alpha, beta, diag;   // C = alpha sum + beta aux + diag on the diagonal; aux nullptr: none
     float* partial;            // [slots][tile]
     uint32_t* counters;        // one per tile that is cut, zero
-    SymCut cut;
+    SymCut cut, diagonal;      // of the tiles; of those of SYM_DIAGONAL, behind tiles of SYM_HALF
     SymPart part;              // at hand
 
     // Quads of outputs (gemm_slim.hpp): the four values of aux, and what becomes of their sums, stored in both places.
@@ -122,7 +157,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t partial_buffer(float* p, int b
 template <typename C, int BM, int BN>
 __device__ __forceinline__ void OrthoSym::finish(const OrthoSym& g, f32x4 (&acc)[C::TM][C::TN], const int i0, const int j0, const int wm, const int wn, const int tid,
                                                  char* smem) {
-    static_assert(BM == BN, "mirror images");
     constexpr int TILE = BM * BN;
     const int lane = tid & 63, wave = wm * (BN / C::WTN) + wn;
     __syncthreads();  // all waves are done reading the operand buffers
@@ -193,7 +227,7 @@ __device__ __forceinline__ void OrthoSym::finish(const OrthoSym& g, f32x4 (&acc)
         for (int b = 0; b < C::TN; ++b)
             *reinterpret_cast<uint2*>(stage + (a * 16 + r) * STRIDE + (b * 16 + c) * 2) = uint2{pack_f16x2(acc[a][b][0], acc[a][b][1]), pack_f16x2(acc[a][b][2], acc[a][b][3])};
     out(IC<C::WTM>{}, IC<C::WTN>{}, row0, col0);
-    if (i0 == j0) return;
+    if (row0 < j0 + BN) return;  // on the diagonal, or above it
 #pragma unroll
     for (int a = 0; a < C::TM; ++a)
 #pragma unroll
@@ -219,20 +253,32 @@ __device__ __forceinline__ void ortho_tile(int t, int& ti, int& tj) {
     while (ti * (ti + 1) / 2 > t) --ti;
     tj = t - ti * (ti + 1) / 2;
 }
+// Tiles of 256 rows and 128 columns: 2 i + 1 of them in the i-th 256 rows, whose last one has the first half of the diagonal; the other half is left to 128 x 128 tiles.
+__device__ __forceinline__ void ortho_half_tile(int t, int& ti, int& tj) {
+    ti = (int)sqrtf((float)t);
+    while ((ti + 1) * (ti + 1) <= t) ++ti;
+    while (ti * ti > t) --ti;
+    tj = t - ti * ti;
+}
+// Of the tiles that `cut` deals out (SIZE: rows), `behind`: not the first ones of the launch.
 template <int SIZE, int LAYOUT>
-__device__ __forceinline__ void ortho_sym(const OrthoSym& args, char* smem) {
-    SymWalk walk(args.cut, xcd_run(blockIdx.x, gridDim.x), gridDim.x);  // neighbours share rows of tiles
+__device__ __forceinline__ void ortho_sym(const OrthoSym& args, const SymCut& cut, char* smem, bool behind = false) {
+    SymWalk walk(cut, xcd_run(blockIdx.x, gridDim.x), gridDim.x);  // neighbours share rows of tiles
     OrthoSym g = args;
-    for (bool first = true; walk.next(args.cut, g.part); first = false) {
+    g.cut = cut;
+    for (bool first = !behind; walk.next(cut, g.part); first = false) {
         g.R = g.part.count * TILE_BK;
         const int64_t skip = (int64_t)g.part.from * TILE_BK * (LAYOUT == KC ? 1 : g.lda);
         g.A = args.A + skip;
         g.B = args.B + skip;
         int ti, tj;
-        ortho_tile(g.part.tile, ti, tj);
+        if constexpr (SIZE == SYM_HALF) ortho_half_tile(g.part.tile, ti, tj);
+        else if constexpr (SIZE == SYM_DIAGONAL) tj = ti = 2 * g.part.tile + 1;
+        else ortho_tile(g.part.tile, ti, tj);
         if (!first) __syncthreads();  // the tile before has left LDS
         if constexpr (SIZE == 64) gemm_ring_body<64, 64, 2, 2, 4, LAYOUT, LAYOUT>(g, ti * 64, tj * 64, smem, threadIdx.x);
-        else if constexpr (SIZE == 128) gemm_ring_body<128, 128, 4, 2, 4, LAYOUT, LAYOUT>(g, ti * 128, tj * 128, smem, threadIdx.x);
+        else if constexpr (SIZE == 128 || SIZE == SYM_DIAGONAL) gemm_ring_body<128, 128, 4, 2, 4, LAYOUT, LAYOUT>(g, ti * 128, tj * 128, smem, threadIdx.x);
+        else if constexpr (SIZE == SYM_HALF) gemm_ring_body<256, 128, 4, 2, 3, LAYOUT, LAYOUT>(g, ti * 256, tj * 128, smem, threadIdx.x);
         else gemm_tile_body<256, 256, 2, 4, LAYOUT, LAYOUT>(g, ti * 256, tj * 256, smem);
     }
 }
@@ -247,17 +293,23 @@ __global__ void __launch_bounds__(SLIM_WAVES * 64) ortho_sym_32_kernel(OrthoSym 
 template <int LAYOUT>
 __global__ void __launch_bounds__(256, 2) ortho_sym_64_kernel(OrthoSym g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    ortho_sym<64, LAYOUT>(g, smem);
+    ortho_sym<64, LAYOUT>(g, g.cut, smem);
 }
 template <int LAYOUT>
 __global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_128_kernel(OrthoSym g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    ortho_sym<128, LAYOUT>(g, smem);
+    ortho_sym<128, LAYOUT>(g, g.cut, smem);
 }
 template <int LAYOUT>
 __global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_256_kernel(OrthoSym g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    ortho_sym<256, LAYOUT>(g, smem);
+    ortho_sym<256, LAYOUT>(g, g.cut, smem);
+}
+template <int LAYOUT>
+__global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_half_kernel(OrthoSym g) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    ortho_sym<SYM_HALF, LAYOUT>(g, g.cut, smem);
+    ortho_sym<SYM_DIAGONAL, LAYOUT>(g, g.diagonal, smem, true);  // (the tiles ahead of them are all taken whole: the sums in the workspace are the diagonal's)
 }
 
 // ---- a step in one launch ----------------------------------------------------------------------

@@ -102,11 +102,20 @@ struct SymKind {
 };
 constexpr SymKind SYM_KINDS[4] = {{64, 1, 0.18, 0.0, 2.9, 1.0, 0.8}, {64, 2, 0.18, 0.13, 3.0, 1.0, 0.8}, {128, 1, 0.32, 0.20, 4.1, 0.5, 1.2}, {256, 1, 1.1, 0.5, 6.0, 2.0, 5.0}};
 constexpr int SYM_MOST_PARTS = 16;  // of a tile
+// Tiles of 256 rows and 128 columns, and the 128 x 128 ones that they leave of the diagonal, both in one launch: `size` of such a plan is SYM_HALF.
+// (The same at half the size, 128 x 64 tiles of which 2048 columns have 256, is slower than 136 whole ones: 96 steps 45 us and 42, 32 steps 21 and 16.  The tiles take in 1.4 times as
+// much, and 10 TB/s of operands already come from the caches.)
+constexpr int SYM_HALF = 257, SYM_DIAGONAL = 129;
 
 struct SymPlan {
     int size = 0, workgroups = 0;
     double us = 1e30;
-    SymCut cut{};
+    SymCut cut{}, diagonal{};
+    int counters() const { return cut.cut + diagonal.cut; }
+    // of the sums that parts of tiles leave
+    int64_t partial_floats() const {
+        return size == SYM_HALF ? (int64_t)diagonal.slots() * (128 * 128) : (int64_t)cut.slots() * size * size;
+    }
 };
 // The quickest of all kinds for s rows and columns, the tiles that do not fill a round taken whole, in slices, or in slices and rests.
 inline SymPlan sym_plan(int64_t s, int64_t steps, int64_t compute_units) {
@@ -116,7 +125,7 @@ inline SymPlan sym_plan(int64_t s, int64_t steps, int64_t compute_units) {
         const int64_t n = (s + 31) / 32, tiles = n * (n + 1) / 2, rounds = (tiles + compute_units - 1) / compute_units;
         const double chain = 0.7 + 0.24 * (double)((steps + 3) / 4);
         const double us = 2.5 + std::max((double)rounds * (0.2 + 0.08 * (double)steps), (double)((rounds + 4) / 5) * chain);
-        if (tiles <= 5 * compute_units) best = {32, (int)tiles, us, {(int)steps, (int)tiles, 0, 1, 0, 0, 0, 1}};
+        if (tiles <= 5 * compute_units) best = {32, (int)tiles, us, {(int)steps, (int)tiles, 0, 1, 0, 0, 0, 1}, {}};
     }
     for (const SymKind& k : SYM_KINDS) {
         const int64_t n = (s + k.size - 1) / k.size, tiles = n * (n + 1) / 2, most = compute_units * k.beside, rounds = tiles / most, left = tiles % most;
@@ -127,7 +136,7 @@ inline SymPlan sym_plan(int64_t s, int64_t steps, int64_t compute_units) {
         };
         const double full_us = k.fixed + walked(rounds * steps, most);
         auto consider = [&](int64_t workgroups, const SymCut& cut, double us) {
-            if (us < best.us) best = {k.size, (int)workgroups, us, cut};
+            if (us < best.us) best = {k.size, (int)workgroups, us, cut, {}};
         };
         consider(std::min(most, tiles), {(int)steps, (int)tiles, 0, 1, 0, 0, 0, 1}, full_us + (left > 0 ? walked(steps, left) : 0.0));
         if (left == 0) continue;
@@ -146,6 +155,18 @@ inline SymPlan sym_plan(int64_t s, int64_t steps, int64_t compute_units) {
             if (q + pieces > SYM_MOST_PARTS) continue;
             consider(most, {(int)steps, whole, cut, (int)q, (int)each, (int)rest, (int)helpers, (int)share},
                      full_us + walked(std::max(each, rest + (further > 0 ? share : 0)), most) + 2.0 * k.leave + (double)(q + pieces) * k.add);
+        }
+    }
+    {   // 256 x 128 tiles, all taken whole, and the diagonal's 128 x 128 ones in up to four slices behind them.  The 256 tiles of 4096 columns: 64 steps 80 us (128 x 128 tiles 92),
+        // 256 steps 255 (256 x 256 ones in slices 282); 4000 columns, 125 steps 130 (128 x 128 ones in slices 147); the 1024 of 8192, 128 steps 485 (256 x 256 ones in slices 480)
+        const int64_t n = (s + 255) / 256, tiles = n * n, rounds = (tiles + compute_units - 1) / compute_units, diagonal = s / 256 + (s % 256 > 128);
+        const int64_t q = std::max<int64_t>(1, std::min<int64_t>({compute_units / std::max<int64_t>(1, diagonal), 4, steps}));
+        const int64_t each = (steps + q - 1) / q, slices = steps / each, rest = steps - slices * each, parts = slices + (rest > 0);
+        const double share = (double)tiles / (double)(rounds * compute_units);
+        const double us = 8.0 + (double)(rounds * steps) * (0.70 + 0.18 * share * share) + (double)each * 0.4 + 1.5 * (double)parts;
+        if (tiles >= compute_units && diagonal * parts <= compute_units && us < best.us) {
+            const SymCut whole{(int)steps, (int)diagonal, 0, 1, 0, 0, 0, 1}, cut{(int)steps, 0, (int)diagonal, (int)slices, (int)each, (int)rest, rest > 0 ? (int)diagonal : 0, 1};
+            best = {SYM_HALF, (int)compute_units, us, {(int)steps, (int)tiles, 0, 1, 0, 0, 0, 1}, parts == 1 ? whole : cut};
         }
     }
     return best;

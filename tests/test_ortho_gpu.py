@@ -80,6 +80,12 @@ def test_places(k, n, wide):
     assert np.array_equal(ortho(g, 4, [1.0, 0.0, 0.0] * 2 + abc + [1.0, 0.0, 0.0], wide), back(half(want * scale) / scale))
 
 
+@pytest.mark.parametrize("k,n", [(3970, 4200), (4300, 3900)])
+def test_places_of_many_tiles(k, n):
+    """More tiles of 128 rows than a round of them takes: others go over the products then."""
+    test_places(k, n, False)
+
+
 @pytest.mark.parametrize("k,n", SHAPES)
 @pytest.mark.parametrize("wide", [False, True])
 def test_five_steps(k, n, wide):
