@@ -58,8 +58,7 @@ class Stream:
         self.update_of = {k: torch.empty_like(self.w[0][k]) for k in MATRICES}
         # a workspace for each purpose: some begin with counters that only their own calls may touch
         sizes = {"gated_up": axo.axo_gated_workspace_bytes(self.up), "gated_down": axo.axo_gated_workspace_bytes(self.down), "norm": axo.axo_norm_workspace_bytes(self.up),
-                 "resnorm": axo.axo_resnorm_workspace_bytes(self.up), "add": axo.axo_fc_add_workspace_bytes(self.down), "ortho_up": axo.axo_ortho_workspace_bytes(self.up),
-                 "ortho_down": axo.axo_ortho_workspace_bytes(self.down)}
+                 "resnorm": axo.axo_resnorm_workspace_bytes(self.up), "add": axo.axo_fc_add_workspace_bytes(self.down), "ortho": max(axo.axo_ortho_workspace_bytes(p) for p in (self.up, self.down))}
         self._forwarded = False  # whether the buffers hold a forward pass
         self._ws = {k: (torch.zeros(max(n, 16), dtype=torch.uint8, device=DEV), n) for k, n in sizes.items()}
 
@@ -124,8 +123,8 @@ class Stream:
         for master, w, grad, momentum in zip(self.master, self.w, self.grad, self.momentum):
             for k, m in momentum.items():
                 m.mul_(kept).add_(grad[k])
-                o, p, name = self.update_of[k], self.down if k == "wd" else self.up, "ortho_down" if k == "wd" else "ortho_up"
-                axo.axo_ortho(p, *_at(m), axo.AXO_TYPE_F32, 5, None, 1e-7, *_at(o), *self._space(name), st)
+                o, p = self.update_of[k], self.down if k == "wd" else self.up
+                axo.axo_ortho(p, *_at(m), axo.AXO_TYPE_F32, 5, None, 1e-7, *_at(o), *self._space("ortho"), st)
                 master[k].add_(o, alpha=-rate)
             for k in master.keys() - momentum.keys():
                 master[k].add_(grad[k], alpha=-rate)

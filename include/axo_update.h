@@ -29,8 +29,8 @@ extern "C" {
  * O: bf16, rounded once.  Between steps X, X X^T and its polynomial are rounded to fp16, X times a power of two; sums are fp32, |G| is formed in fp64.  For G with singular values
  * within a factor of a hundred O is off by about 0.1 % before its rounding to bf16 (0.2 %).  What of G lies further below its largest singular value, by a factor of a thousand
  * or more, is taken up with what rounding adds there.  Results are a fixed function of the inputs.
- * ws: axo_ortho_workspace_bytes(p) bytes of device memory, 16-byte aligned.  It begins with arrival counters: zero-fill it once after allocating it and leave it to
- * calls of axo_ortho with the same sizes, which must not overlap in time on one workspace.
+ * ws: axo_ortho_workspace_bytes(p) bytes or more of device memory, 16-byte aligned.  It begins with arrival counters: zero-fill it once after allocating it and leave it to
+ * calls of axo_ortho, of any sizes that it is large enough for, which must not overlap in time on one workspace.
  * Errors: those of axo_shard_dims; BAD_GRID; BAD_ARG (type, steps, coefficients or eps, shared bytes); NULL_PTR, BAD_LD, MISALIGNED; BAD_SIZE (K N of 2^31 and more, each
  * rounded up to 64); WORKSPACE; HIP. */
 int axo_ortho(const axo_problem_t *p, const void *G, int64_t ldg, int type, int steps, const float *abc, float eps, void *O, int64_t ldo, void *ws,

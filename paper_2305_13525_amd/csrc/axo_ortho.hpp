@@ -43,7 +43,7 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
         return from;
     };
     auto partials = [](const axo::SymPlan& y) { return (size_t)y.partial_floats() * sizeof(float); };
-    p->counters = take((size_t)std::max(p->gram.counters(), p->poly.counters()) * sizeof(uint32_t));
+    p->counters = take((size_t)axo::SYM_MOST_CUT * sizeof(uint32_t));  // where and as many as for any other sizes
     p->sums = take(axo::ORTHO_SUMS * sizeof(double));
     p->A = take((size_t)(p->s * p->s) * 2);
     p->Q = take((size_t)(p->s * p->s) * 2);

@@ -102,6 +102,7 @@ struct SymKind {
 };
 constexpr SymKind SYM_KINDS[4] = {{64, 1, 0.18, 0.0, 2.9, 1.0, 0.8}, {64, 2, 0.18, 0.13, 3.0, 1.0, 0.8}, {128, 1, 0.32, 0.20, 4.1, 0.5, 1.2}, {256, 1, 1.1, 0.5, 6.0, 2.0, 5.0}};
 constexpr int SYM_MOST_PARTS = 16;  // of a tile
+constexpr int SYM_MOST_CUT = 512;   // tiles that are cut: fewer than workgroups beside each other on 256 compute units
 // Tiles of 256 rows and 128 columns, and the 128 x 128 ones that they leave of the diagonal, both in one launch: `size` of such a plan is SYM_HALF.
 // (The same at half the size, 128 x 64 tiles of which 2048 columns have 256, is slower than 136 whole ones: 96 steps 45 us and 42, 32 steps 21 and 16.  The tiles take in 1.4 times as
 // much, and 10 TB/s of operands already come from the caches.)

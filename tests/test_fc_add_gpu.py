@@ -51,6 +51,12 @@ def check_forward(d, epilogue, wide, save=False, gap=0, p=None, scale=SCALE, add
         bu.within(Z, z, bz, "z")
 
 
+@pytest.mark.parametrize("m,k,n", [(1, 6400, 8192), (5, 8208, 6424), (16, 16384, 3208), (3, 5000, 5000), (9, 3500, 8000)])
+def test_few_tokens_and_much_weight(m, k, n):
+    """Weights that are read from memory, beyond 100 MB by rows of 256 bytes."""
+    check_forward(inputs(m, k, n, m + k, m % 2 == 1), 1 + m % 3, m % 2 == 1, gap=8)
+
+
 @pytest.mark.parametrize("m,k,n", SIZES)
 @pytest.mark.parametrize("wide", [False, True])
 def test_forward(m, k, n, wide):

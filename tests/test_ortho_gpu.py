@@ -113,6 +113,27 @@ def test_singular_values():
     assert np.abs(m - np.diag(np.diag(m))).max() < 0.02
 
 
+@pytest.mark.parametrize("wide,exponent", [(True, -140), (True, 120), (False, -130), (False, 120)])
+def test_any_magnitude(wide, exponent):
+    """A power of two in G changes nothing, down to subnormal values and up to squares that fp32 does not hold: the same bits."""
+    rng = np.random.default_rng(9)
+    for k, n in [(40, 72), (300, 517)]:
+        g = rng.integers(-3, 4, (k, n)).astype(np.float64)
+        assert np.array_equal(ortho(g * 2.0 ** exponent, wide=wide), ortho(g, wide=wide))
+
+
+def test_one_workspace_for_all_sizes():
+    """Calls of several sizes, whose products are cut in different ways, one behind the other on one workspace."""
+    rng = np.random.default_rng(10)
+    sizes = [(1024, 4096), (515, 259), (1500, 6144), (64, 64), (200, 900)]
+    kept = max((workspace(bu.problem(0, k, n)) for k, n in sizes), key=lambda w: w[1])
+    g = [bu.draw(rng, k, n) for k, n in sizes]
+    want = [ortho(v) for v in g]
+    for _ in range(2):
+        for v, w in zip(g, want):
+            assert np.array_equal(ortho(v, kept=kept), w)
+
+
 def test_coefficients_of_each_step():
     rng = np.random.default_rng(2)
     g = bu.draw(rng, 100, 180)

@@ -75,7 +75,9 @@ int main() {
         for (long s : {1, 64, 128, 192, 576, 640, 1024, 1088, 1536, 2048, 2112, 3904, 4032, 4096, 4160, 5696})
             for (long steps : {1, 2, 3, 7, 9, 16, 17, 32, 33, 64, 100, 255, 256}) {
                 if (units == 7 && s > 1100) continue;
-                check(s, steps, units, axo::sym_plan(s, steps, units));
+                const axo::SymPlan plan = axo::sym_plan(s, steps, units);
+                check(s, steps, units, plan);
+                CHECK(plan.counters() <= axo::SYM_MOST_CUT);
                 ++n;
             }
         for (long cut = 1; cut < units; cut += units > 100 ? 5 : 1)  // slices and rests of any proportion, whether they are planned or not
