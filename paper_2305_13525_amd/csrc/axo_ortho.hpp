@@ -20,6 +20,7 @@ struct OrthoPlan {
     bool tall;       // more rows than columns
     int exponent;    // X is held as its values times 2^exponent
     bool at_once;    // a step is one launch
+    bool rest;       // a step is two, gram and the rest
     axo::SymPlan gram, poly;
     size_t counters, sums, A, Q, X[2], partial, bytes;  // offsets in the workspace
 };
@@ -36,6 +37,7 @@ int make_plan(const Shard& sh, OrthoPlan* p) {
     p->gram = axo::sym_plan(p->s, p->l / axo::TILE_BK, NUM_CU);
     p->poly = axo::sym_plan(p->s, p->s / axo::TILE_BK, NUM_CU);
     p->at_once = p->s <= 128 && p->s * p->l <= axo::ORTHO_STEP_MOST;
+    p->rest = p->s <= 128 && p->s * p->l <= axo::ORTHO_REST_MOST;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t from = at;
@@ -58,12 +60,13 @@ struct SymHalfCfg {
     static constexpr int THREADS = axo::TILE_THREADS, LDS_BYTES = std::max(axo::MixSmallCfg::LDS_BYTES, axo::MidCfg::LDS_BYTES);
     static_assert(axo::MixSmallCfg::THREADS == THREADS && axo::MidCfg::THREADS == THREADS, "one launch");
 };
-template <int SIZE, int LAYOUT>
+template <int SIZE, int LAYOUT, bool SLICED = false>
 int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
-    using C = std::conditional_t<SIZE == 32, axo::SlimCfg<32, 32, axo::SLIM_WAVES, 1>, std::conditional_t<SIZE == 64, axo::SmallCfg<false>,
+    using C = std::conditional_t<SIZE == 32, axo::SlimCfg<32, 32, axo::SLIM_WAVES, SLICED ? axo::SLICED_STAGES : 1>, std::conditional_t<SIZE == 64, axo::SmallCfg<false>,
         std::conditional_t<SIZE == 128, axo::MidCfg, std::conditional_t<SIZE == axo::SYM_HALF, SymHalfCfg, axo::MixBigCfg>>>>;
     auto kern = [] {
-        if constexpr (SIZE == 32) return axo::ortho_sym_32_kernel<LAYOUT>;
+        if constexpr (SIZE == 32 && SLICED) return axo::ortho_sym_32_sliced_kernel<LAYOUT>;
+        else if constexpr (SIZE == 32) return axo::ortho_sym_32_kernel<LAYOUT>;
         else if constexpr (SIZE == 64) return axo::ortho_sym_64_kernel<LAYOUT>;
         else if constexpr (SIZE == 128) return axo::ortho_sym_128_kernel<LAYOUT>;
         else if constexpr (SIZE == axo::SYM_HALF) return axo::ortho_sym_half_kernel<LAYOUT>;
@@ -77,6 +80,7 @@ int launch_sym(const axo::OrthoSym& g, int workgroups, hipStream_t st) {
 int launch_sym(axo::OrthoSym g, const axo::SymPlan& y, bool tall, hipStream_t st) {
     g.cut = y.cut;
     g.diagonal = y.diagonal;
+    if (y.size == 32 && y.cut.cut > 0) return tall ? launch_sym<32, axo::MC, true>(g, y.workgroups, st) : launch_sym<32, axo::KC, true>(g, y.workgroups, st);
     if (y.size == 32) return tall ? launch_sym<32, axo::MC>(g, y.workgroups, st) : launch_sym<32, axo::KC>(g, y.workgroups, st);
     if (y.size == 64) return tall ? launch_sym<64, axo::MC>(g, y.workgroups, st) : launch_sym<64, axo::KC>(g, y.workgroups, st);
     if (y.size == axo::SYM_HALF) return tall ? launch_sym<axo::SYM_HALF, axo::MC>(g, y.workgroups, st) : launch_sym<axo::SYM_HALF, axo::KC>(g, y.workgroups, st);
@@ -114,6 +118,15 @@ int launch_step(const axo::OrthoStep& g, hipStream_t st) {
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.R / 64)), dim3(C::THREADS), C::LDS_BYTES, st, g);
     return launched();
 }
+template <int S>
+int launch_rest(const axo::OrthoStep& g, const bf16_t* gram, hipStream_t st) {
+    using C = std::conditional_t<S == 64, axo::SmallCfg<false>, axo::MidCfg>;
+    auto kern = axo::ortho_rest_kernel<S>;
+    static std::atomic<uint64_t> raised{0};
+    if (!raise_lds_limit(reinterpret_cast<const void*>(kern), C::LDS_BYTES, &raised)) return AXO_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.R / 64)), dim3(C::THREADS), C::LDS_BYTES, st, g, gram);
+    return launched();
+}
 template <typename T>
 int launch_load(const axo::OrthoLoadArgs& g, hipStream_t st) {
     hipLaunchKernelGGL(axo::ortho_norm_kernel<T>, dim3(axo::ORTHO_SUMS), dim3(axo::ORTHO_THREADS), 0, st, g);
@@ -141,13 +154,14 @@ int ortho(const OrthoPlan& pl, const axo::OrthoLoadArgs& from, int type, int ste
     for (int i = 0; i < steps; ++i) {
         const float* const c = abc ? abc + 3 * i : QUINTIC;
         const bf16_t* const x = X[i % 2];
-        if (pl.at_once) {
-            axo::OrthoStep y{};
+        axo::OrthoStep whole{};
+        if (pl.at_once || pl.rest) {
+            axo::OrthoStep& y = whole;
             y.A = y.B = x;
             y.lda = y.ldb = load.cols;
             y.C = X[(i + 1) % 2]; y.ldc = load.cols;
             y.Mo = y.No = s; y.R = l;
-            y.alpha = (float)std::ldexp(1.0, -2 * pl.exponent);
+            y.alpha = pl.at_once ? (float)std::ldexp(1.0, -2 * pl.exponent) : 1.0f;  // of A, which gram has left with it
             y.a = c[0]; y.b = c[1]; y.c = c[2];
             y.scale = (float)std::ldexp(1.0, -pl.exponent);
             y.K = from.K; y.N = from.N;
@@ -156,6 +170,9 @@ int ortho(const OrthoPlan& pl, const axo::OrthoLoadArgs& from, int type, int ste
                 y.O = O;
                 y.ldo = ldo;
             }
+        }
+        if (pl.at_once) {
+            const axo::OrthoStep& y = whole;
             if (const int rc = s == 64 ? (pl.tall ? launch_step<64, axo::MC>(y, st) : launch_step<64, axo::KC>(y, st))
                                        : (pl.tall ? launch_step<128, axo::MC>(y, st) : launch_step<128, axo::KC>(y, st)))
                 return rc;
@@ -170,6 +187,10 @@ int ortho(const OrthoPlan& pl, const axo::OrthoLoadArgs& from, int type, int ste
         y.partial = reinterpret_cast<float*>(ws + pl.partial);
         y.counters = reinterpret_cast<uint32_t*>(ws + pl.counters);
         if (const int rc = launch_sym(y, pl.gram, pl.tall, st)) return rc;
+        if (pl.rest) {
+            if (const int rc = s == 64 ? launch_rest<64>(whole, A, st) : launch_rest<128>(whole, A, st)) return rc;
+            continue;
+        }
         y.A = y.B = A;
         y.lda = y.ldb = s;
         y.C = Q;

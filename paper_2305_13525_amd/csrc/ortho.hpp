@@ -240,7 +240,12 @@ __device__ __forceinline__ void OrthoSym::finish(const OrthoSym& g, f32x4 (&acc)
     out(IC<C::WTN>{}, IC<C::WTM>{}, col0, row0);
 }
 
+// (Of 32 x 32 tiles: a part leaves its sums by thread.)
 __device__ __forceinline__ void OrthoSym::quad(const OrthoSym& g, bool mirrored, int row, int col, f32x4 sum, uint2 raw) {
+    if (g.part.cut >= 0) {
+        const __amdgpu_buffer_rsrc_t mine = partial_buffer(g.partial + (int64_t)g.part.slot * 1024, 4096);
+        return __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sum), mine, threadIdx.x * 16, 0, DEVICE_SCOPE);
+    }
     const f32x4 v = g.value(row, col, sum, raw);
     *reinterpret_cast<uint2*>(g.C + (int64_t)row * g.ldc + col) = uint2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
     if (!mirrored) return;
@@ -290,7 +295,50 @@ __global__ void __launch_bounds__(SLIM_WAVES * 64) ortho_sym_32_kernel(OrthoSym 
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     int ti, tj;
     ortho_tile(xcd_run(blockIdx.x, gridDim.x), ti, tj);
+    g.part.cut = -1;
     slim_tile_body<32, 32, SLIM_WAVES, 1, LAYOUT, LAYOUT>(g, ti * 32, tj * 32, threadIdx.x, smem);
+}
+// The same, a slice of a tile to a workgroup; a quad of the output to a thread.  Two chunks under way to a wave: an X that is not in the L2 is waited for (128 x 65536, five steps, 183 us, with one 196).
+// Before there were slices the update of 64 x 4096 took 87 us and takes 56, 128 x 16384 110 and 94, 256 x 4096 104 and 90.
+constexpr int SLICED_STAGES = 2;
+template <int LAYOUT>
+__global__ void __launch_bounds__(SLIM_WAVES * 64) ortho_sym_32_sliced_kernel(OrthoSym args) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    static_assert(SLIM_WAVES * 64 * 4 == 32 * 32, "a quad to a thread");
+    OrthoSym g = args;
+    SymWalk walk(g.cut, xcd_run(blockIdx.x, gridDim.x), gridDim.x);
+    if (!walk.next(g.cut, g.part)) return;
+    g.R = g.part.count * TILE_BK;
+    const int64_t skip = (int64_t)g.part.from * TILE_BK * (LAYOUT == KC ? 1 : g.lda);
+    g.A = args.A + skip;
+    g.B = args.B + skip;
+    int ti, tj;
+    ortho_tile(g.part.tile, ti, tj);
+    slim_tile_body<32, 32, SLIM_WAVES, SLICED_STAGES, LAYOUT, LAYOUT>(g, ti * 32, tj * 32, threadIdx.x, smem);
+    if (g.part.cut < 0) return;  // the only part of its tile
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // as OrthoSym::finish
+    __syncthreads();
+    uint32_t* const arrived = reinterpret_cast<uint32_t*>(smem);
+    if (threadIdx.x == 0) *arrived = __hip_atomic_fetch_add(g.counters + g.part.cut, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (*arrived != (uint32_t)(g.part.parts - 1)) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int part = 0; part < g.part.parts; part += 8) {  // eight requested at a time
+        f32x4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (part + i < g.part.parts)
+                v[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(partial_buffer(g.partial + (int64_t)g.cut.slot_of(g.part.cut, part + i) * 1024, 4096),
+                                                                                       threadIdx.x * 16, 0, DEVICE_SCOPE));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i];
+    }
+    if (threadIdx.x == 0) __hip_atomic_store(g.counters + g.part.cut, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    g.part.cut = -1;
+    const int row = ti * 32 + (int)threadIdx.x / 8, col = tj * 32 + (int)threadIdx.x % 8 * 4;
+    OrthoSym::quad(g, ti != tj, row, col, sum, OrthoSym::request(g, row, col));
 }
 template <int LAYOUT>
 __global__ void __launch_bounds__(256, 2) ortho_sym_64_kernel(OrthoSym g) {
@@ -317,9 +365,9 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) ortho_sym_half_kernel(OrthoSy
 // ---- a step in one launch ----------------------------------------------------------------------
 // Where s is at most 128 the three products of a step are too small to be worth a launch each: 3 to 4 us apiece, of which the matrix units work a tenth.  A workgroup here
 // has a slab of 64 of the l columns (rows, of a tall X) of the next X, and forms the whole of A for itself, as one tile of S x S; A, Q and the slab of X then go through LDS
-// only.  Every workgroup does the same l / 64 steps of A, so this is for X of up to ORTHO_STEP_MOST values.  Five steps with three launches each and with one: 128 x 512 65 and 48 us,
-// 128 x 2048 some 75 and 84.
-constexpr int ORTHO_STEP_MOST = 128 * 1024;
+// only.  Every workgroup does the same l / 64 steps of A, so this is for X of up to ORTHO_STEP_MOST values; to ORTHO_REST_MOST gram is a launch of its own (ortho_rest_kernel).
+// Five steps with three launches each, with two and with one: 128 x 512 65 us, 60 and 48; 128 x 2048 78, 73 and 84; 64 x 4096 73 and 56, 128 x 16384 103 and 94, 128 x 32768 110 and 130.
+constexpr int ORTHO_STEP_MOST = 128 * 1024, ORTHO_REST_MOST = 128 * 16384;
 struct OrthoStep : GemmArgs {
     static constexpr bool F16 = true, OWN = true;
     float alpha;             // of A
@@ -459,6 +507,24 @@ __global__ void __launch_bounds__(S * 4, 1) ortho_step_kernel(OrthoStep g) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     if constexpr (S == 64) gemm_ring_body<64, 64, 2, 2, 4, LAYOUT, LAYOUT>(g, 0, 0, smem, threadIdx.x);
     else gemm_ring_body<128, 128, 4, 2, 4, LAYOUT, LAYOUT>(g, 0, 0, smem, threadIdx.x);
+}
+
+// The same behind a gram launch, where l is longer: a workgroup reads A instead.
+template <int S>
+__global__ void __launch_bounds__(S * 4, S == 64 ? 2 : 1) ortho_rest_kernel(OrthoStep g, const bf16_t* gram) {
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    using C = std::conditional_t<S == 64, RingCfg<64, 64, 2, 2, 4>, RingCfg<128, 128, 4, 2, 4>>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+    f32x4 acc[C::TM][C::TN];
+#pragma unroll
+    for (int a = 0; a < C::TM; ++a)
+#pragma unroll
+        for (int b = 0; b < C::TN; ++b) {
+            const uint2 raw = *reinterpret_cast<const uint2*>(gram + (wm * C::WTM + a * 16 + (lane & 15)) * S + wn * C::WTN + b * 16 + 4 * (lane >> 4));
+            const f16x2 lo = __builtin_bit_cast(f16x2, raw.x), hi = __builtin_bit_cast(f16x2, raw.y);
+            acc[a][b] = f32x4{(float)lo[0], (float)lo[1], (float)hi[0], (float)hi[1]};
+        }
+    OrthoStep::finish<C, S, S>(g, acc, 0, 0, wm, wn, threadIdx.x, smem);
 }
 
 // ---- apply --------------------------------------------------------------------------------------

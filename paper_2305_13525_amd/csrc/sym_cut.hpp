@@ -127,6 +127,12 @@ inline SymPlan sym_plan(int64_t s, int64_t steps, int64_t compute_units) {
         const double chain = 0.7 + 0.24 * (double)((steps + 3) / 4);
         const double us = 2.5 + std::max((double)rounds * (0.2 + 0.08 * (double)steps), (double)((rounds + 4) / 5) * chain);
         if (tiles <= 5 * compute_units) best = {32, (int)tiles, us, {(int)steps, (int)tiles, 0, 1, 0, 0, 0, 1}, {}};
+        for (int64_t q = 2; q <= SYM_MOST_PARTS && q * tiles <= compute_units && 4 * q <= steps; ++q) {
+            const int64_t each = (steps + q - 1) / q, slices = steps / each, rest = steps - slices * each, parts = slices + (rest > 0);
+            const double sliced = 2.5 + std::max(0.2 + 0.08 * (double)each, 0.7 + 0.24 * (double)((each + 3) / 4)) + 1.5 + 0.1 * (double)parts;
+            if (sliced < best.us)
+                best = {32, (int)(tiles * parts), sliced, {(int)steps, 0, (int)tiles, (int)slices, (int)each, (int)rest, rest > 0 ? (int)tiles : 0, 1}, {}};
+        }
     }
     for (const SymKind& k : SYM_KINDS) {
         const int64_t n = (s + k.size - 1) / k.size, tiles = n * (n + 1) / 2, most = compute_units * k.beside, rounds = tiles / most, left = tiles % most;

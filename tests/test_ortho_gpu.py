@@ -45,7 +45,7 @@ def hadamard(n):
 
 # rows x columns: below a tile, whole tiles, ragged ones, wide and tall, products of several workgroups to a tile and of several tiles to a workgroup
 SHAPES = [(1, 1), (1, 9), (7, 3), (40, 40), (64, 64), (65, 64), (64, 130), (130, 70), (128, 512), (200, 200), (515, 259), (257, 1000), (64, 4096), (3000, 72), (1000, 1030),
-          (640, 2500), (2049, 1500)]
+          (640, 2500), (2049, 1500), (60, 5000), (6000, 100), (128, 17000), (250, 4500), (9000, 200)]
 
 
 @pytest.mark.parametrize("k,n", SHAPES)
@@ -125,7 +125,7 @@ def test_any_magnitude(wide, exponent):
 def test_one_workspace_for_all_sizes():
     """Calls of several sizes, whose products are cut in different ways, one behind the other on one workspace."""
     rng = np.random.default_rng(10)
-    sizes = [(1024, 4096), (515, 259), (1500, 6144), (64, 64), (200, 900)]
+    sizes = [(1024, 4096), (515, 259), (1500, 6144), (64, 64), (200, 900), (100, 6000), (7000, 250)]
     kept = max((workspace(bu.problem(0, k, n)) for k, n in sizes), key=lambda w: w[1])
     g = [bu.draw(rng, k, n) for k, n in sizes]
     want = [ortho(v) for v in g]
