@@ -136,6 +136,25 @@ def test_operands_past_4_gib():
     bu.within(Y.result(), y, ru.fc_add_bounds(d["x"], d["w"], d["r"], z, y, SCALE, 1, False)[0])
 
 
+@pytest.mark.parametrize("m,k,n", [(3, 72, 40), (3, 4096, 72)])
+def test_stream_past_4_gib(m, k, n):
+    """Rows of R, Y, Z and of the gradients a billion elements apart."""
+    d, ld = inputs(m, k, n, 12, False), (1 << 30) + 8
+    far = [torch.empty((m - 1) * ld + 1024, dtype=torch.bfloat16, device=bu.DEV) for _ in range(4)]
+    R, Y, Z, dZ = (t.as_strided((m, n), (ld, 1)) for t in far)
+    R.copy_(torch.from_numpy(d["r"]).bfloat16())
+    X, W, p, bias = bu.Mat(d["x"]), bu.Mat(d["w"]), bu.problem(m, k, n), bu.vec(d["bias"])
+    size = axo.axo_fc_add_workspace_bytes(p)
+    ws = torch.zeros(max(size, 16), dtype=torch.uint8, device=bu.DEV)
+    axo.axo_fc_add(p, X.ptr, X.ld, W.ptr, W.ld, bias.data_ptr(), 2, far[0].data_ptr(), ld, 0, SCALE, far[2].data_ptr(), ld, far[1].data_ptr(), ld, ws.data_ptr(), size, bu.stream())
+    y, z = forward(d, 2, False, save=True)
+    back = lambda t: t.double().cpu().numpy()  # noqa: E731
+    assert np.array_equal(back(Y), y) and np.array_equal(back(Z), z)
+    axo.axo_fc_add_dact(p, far[0].data_ptr(), ld, 0, far[2].data_ptr(), ld, 2, SCALE, far[3].data_ptr(), ld, bu.stream())
+    want = SCALE * d["r"] * orr.act(z, 2)[1]
+    bu.within(back(dZ), want, ru.dact_bound(d["r"], z, SCALE, 2, want))
+
+
 @pytest.mark.parametrize("m,n", [(1, 1), (1, 8), (3, 7), (70, 333), (257, 1024), (1000, 520)])
 @pytest.mark.parametrize("wide", [False, True])
 def test_gradient(m, n, wide):

@@ -122,6 +122,20 @@ def test_any_magnitude(wide, exponent):
         assert np.array_equal(ortho(g * 2.0 ** exponent, wide=wide), ortho(g, wide=wide))
 
 
+def test_offsets_past_32_bits():
+    """Rows of G and O a billion elements apart."""
+    ld = (1 << 30) + 8
+    for k, n in ((3, 1000), (3, 70)):
+        g = bu.draw(np.random.default_rng(11), k, n)
+        far = [torch.empty((k - 1) * ld + 1024, dtype=torch.bfloat16, device=bu.DEV) for _ in range(2)]
+        rows = [t.as_strided((k, n), (ld, 1)) for t in far]
+        rows[0].copy_(torch.from_numpy(g).bfloat16())
+        p = bu.problem(0, k, n)
+        ws, size = workspace(p)
+        axo.axo_ortho(p, far[0].data_ptr(), ld, 0, 5, None, 0.0, far[1].data_ptr(), ld, ws.data_ptr(), size, bu.stream())
+        assert np.array_equal(rows[1].double().cpu().numpy(), ortho(g))
+
+
 def test_one_workspace_for_all_sizes():
     """Calls of several sizes, whose products are cut in different ways, one behind the other on one workspace."""
     rng = np.random.default_rng(10)

@@ -239,6 +239,28 @@ def test_offsets_past_32_bits():
     assert np.array_equal(rows[1].double().cpu().numpy(), S) and np.array_equal(Y.result(), Yw) and np.array_equal(st.double().cpu().numpy(), stw)
 
 
+@pytest.mark.parametrize("k", [1000, 17000])
+def test_backward_offsets_past_32_bits(k):
+    """Rows of all matrices a billion elements apart."""
+    m, ld = 3, (1 << 30) + 8
+    d = inputs(m, k, False, 19)
+    p = bu.problem(m, k, 0)
+    (S, stats), want = backward(d, (1, 1), False)
+    far = [torch.empty(2 * ld + 17408, dtype=torch.bfloat16, device=bu.DEV) for _ in range(6)]
+    rows = [t.as_strided((m, k), (ld, 1)) for t in far]
+    for r, v in zip(rows, (d["dy"], d["ds"], d["b"], S)):
+        r.copy_(torch.from_numpy(v).bfloat16())
+    dev, _ = vectors(d)
+    out = [torch.zeros(k, device=bu.DEV) for _ in GRADS]
+    ws = torch.empty(axo.axo_resnorm_workspace_bytes(p), dtype=torch.uint8, device=bu.DEV)
+    stats = torch.from_numpy(stats).float().to(bu.DEV)
+    at = [t.data_ptr() for t in far]
+    axo.axo_resnorm_bwd(p, at[0], ld, at[1], ld, at[2], ld, at[3], ld, 0, 1, bu.ptr(dev["gamma_a"]), bu.ptr(dev["beta_a"]), bu.ptr(dev["gate"]), SCALE, 1, bu.ptr(dev["gamma_b"]),
+                        stats.data_ptr(), at[4], ld, at[5], ld, *[t.data_ptr() for t in out], 0, ws.data_ptr(), ws.numel(), bu.stream())
+    got = [rows[4], rows[5]] + out
+    assert all(np.array_equal(a.double().cpu().numpy(), b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("m,k", [(1, 4096), (37, 1027), (700, 512), (64, 12288), (3, 17000)])
 def test_same_bits_on_any_stream_and_in_graphs(m, k):
     d = inputs(m, k, False, 18)
