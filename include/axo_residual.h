@@ -74,7 +74,7 @@ int axo_resnorm_bwd(const axo_problem_t *p, const void *dY, int64_t lddy, const 
                     const float *stats, void *dX, int64_t lddx, void *dB, int64_t lddb, float *dgamma_a, float *dbeta_a, float *dgate, float *dgamma_b,
                     float *dbeta_b, int accumulate, void *ws, size_t ws_bytes, void *hip_stream);
 
-/* Host only.  Bytes of device workspace that axo_resnorm_bwd needs for this problem; 0 for an invalid one. */
+/* Host only.  Bytes of device workspace that axo_resnorm_bwd needs for this problem; 0 for one that it refuses. */
 size_t axo_resnorm_workspace_bytes(const axo_problem_t *p);
 
 #ifdef __cplusplus

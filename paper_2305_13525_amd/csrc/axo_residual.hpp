@@ -219,7 +219,7 @@ int axo_resnorm_bwd(const axo_problem_t* p, const void* dY, int64_t lddy, const 
 
 size_t axo_resnorm_workspace_bytes(const axo_problem_t* p) {
     axo_host::Shard s;
-    return axo_host::derive_shard(p, &s) ? 0 : axo_block::resnorm_workspace(s.M, s.Kl);
+    return axo_host::derive_shard(p, &s) || axo_block::k_axis(p) != 1 ? 0 : axo_block::resnorm_workspace(s.M, s.Kl);
 }
 
 int axo_fc_add(const axo_problem_t* p, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* bias, int epilogue, const void* R, int64_t ldr, int type,
