@@ -31,8 +31,8 @@ extern "C" {
  * or more, is taken up with what rounding adds there.  Results are a fixed function of the inputs.
  * ws: axo_ortho_workspace_bytes(p) bytes or more of device memory, 16-byte aligned.  It begins with arrival counters: zero-fill it once after allocating it and leave it to
  * calls of axo_ortho, of any sizes that it is large enough for, which must not overlap in time on one workspace.
- * Errors: those of axo_shard_dims; BAD_GRID; BAD_ARG (type, steps, coefficients or eps, shared bytes); NULL_PTR, BAD_LD, MISALIGNED; BAD_SIZE (K N of 2^31 and more, each
- * rounded up to 64); WORKSPACE; HIP. */
+ * Errors: those of axo_shard_dims; BAD_GRID; BAD_ARG (type, steps, coefficients or eps, shared bytes); NULL_PTR, BAD_LD, MISALIGNED; BAD_SIZE (a weight
+ * is taken with s (l + 256) below 2^31 - 2^15, s the smaller and l the larger of K and N, each rounded up to 64); WORKSPACE; HIP. */
 int axo_ortho(const axo_problem_t *p, const void *G, int64_t ldg, int type, int steps, const float *abc, float eps, void *O, int64_t ldo, void *ws,
               size_t ws_bytes, void *hip_stream);
 
