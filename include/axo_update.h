@@ -26,9 +26,9 @@ extern "C" {
  * G: of `type` (axo_type_t).  abc: 3 * steps floats in HOST memory, read before the call returns, (a, b, c) of each step; NULL: (3.4445, -4.7750, 2.0315) in all, of which five
  * steps bring singular values from 0.01 on to between 0.6 and 1.3.  The coefficients have to keep singular values below 2: X is held in fp16 between steps.  eps >= 0 and
  * finite.  A G of zeros gives zeros.  A G with an infinity or a NaN gives NaN.
- * O: bf16, rounded once.  Between steps X, X X^T and its polynomial are rounded to fp16, X times a power of two; sums are fp32, |G| is formed in fp64.  For G with singular values
- * within a factor of a hundred O is off by about 0.1 % before its rounding to bf16 (0.2 %).  What of G lies further below its largest singular value, by a factor of a thousand
- * or more, is taken up with what rounding adds there.  Results are a fixed function of the inputs.
+ * O: bf16, rounded once.  Between steps X, X X^T and its polynomial are rounded to fp16, X times a power of two; sums are fp32, |G| is formed in fp64.  Before its rounding to bf16
+ * (0.2 %) O is off by 0.1 to 0.2 % for random G, and, what rounding adds being taken up along with G's small singular values, for G whose singular values lie evenly in their logarithm
+ * over a factor of 10 by 0.1 %, 30 0.2, 100 0.2 to 0.4, 1000 0.3 to 1.1 (five steps; with X, X X^T and its polynomial in bf16 eight times as much).  Results are a fixed function of the inputs.
  * ws: axo_ortho_workspace_bytes(p) bytes or more of device memory, 16-byte aligned.  It begins with arrival counters: zero-fill it once after allocating it and leave it to
  * calls of axo_ortho, of any sizes that it is large enough for, which must not overlap in time on one workspace.
  * Errors: those of axo_shard_dims; BAD_GRID; BAD_ARG (type, steps, coefficients or eps, shared bytes); NULL_PTR, BAD_LD, MISALIGNED; BAD_SIZE (a weight

@@ -5,9 +5,11 @@
 //   poly   Q of A           s x s of s                    likewise, A read in the epilogue
 //   apply  X <- Q X         s x l of s                    tiles of gemm_tile.hpp
 // (s the smaller of G's sizes, l the larger), bound by the matrix units.  Nothing is rounded to bf16 on the way: the iteration brings small singular values up, and what
-// rounding adds along with them, 1 % of the result with X, A and Q in bf16.  They are held in fp16, which the matrix units take at the same rate, X with a power of two
-// that keeps its values off the subnormal numbers (its largest singular value is about 1, so its values are of 1 / sqrt(K N) or more): 0.1 %, and 0.2 % with the last rounding
-// to bf16.  Sums are fp32, the norm of G is summed up in fp64, where no square leaves the range.  `a` goes into Q's diagonal, so that X is read once.
+// rounding adds along with them, of a random G 0.7 to 1.4 % of the result with X, A and Q in bf16.  They are held in fp16, which the matrix units take at the same rate, X with a power of two
+// that keeps its values off the subnormal numbers (its largest singular value is about 1, so its values are of 1 / sqrt(K N) or more): 0.1 to 0.2 %, and 0.2 to 0.25 % with the last
+// rounding to bf16.  Both grow with the spread of G's singular values, in which X's rounding is more beside the small ones: evenly in their logarithm over a factor of 100, 1.6 to 3.2 % in bf16
+// and 0.2 to 0.4 in fp16, of 1000 2.8 to 8.4 and 0.3 to 1.1.
+// Sums are fp32, the norm of G is summed up in fp64, where no square leaves the range.  `a` goes into Q's diagonal, so that X is read once.
 // All matrices here are padded with zeros to whole multiples of 64, so that inside no product has an edge within a chunk of eight; the padding stays zero.
 #pragma once
 #include "axo_common.hpp"
