@@ -43,7 +43,7 @@ def hadamard(n):
     return h
 
 
-# rows x columns: below a tile, whole tiles, ragged ones, wide and tall, products of several workgroups to a tile and of several tiles to a workgroup
+# rows x columns: below a tile, whole tiles, ragged ones, wide and tall, products of several workgroups to a tile (every other way of dealing tiles out: ortho_plans.py)
 SHAPES = [(1, 1), (1, 9), (7, 3), (40, 40), (64, 64), (65, 64), (64, 130), (130, 70), (128, 512), (200, 200), (515, 259), (257, 1000), (64, 4096), (3000, 72), (1000, 1030),
           (640, 2500), (2049, 1500), (60, 5000), (6000, 100), (128, 17000), (250, 4500), (9000, 200)]
 
