@@ -10,7 +10,8 @@
 // rounding to bf16.  Both grow with the spread of G's singular values, in which X's rounding is more beside the small ones: evenly in their logarithm over a factor of 100, 1.6 to 3.2 % in bf16
 // and 0.2 to 0.4 in fp16, of 1000 2.8 to 8.4 and 0.3 to 1.1.
 // Sums are fp32, the norm of G is summed up in fp64, where no square leaves the range.  `a` goes into Q's diagonal, so that X is read once.
-// All matrices here are padded with zeros to whole multiples of 64, so that inside no product has an edge within a chunk of eight; the padding stays zero.
+// All matrices here are padded to whole multiples of 64, so that inside no product has an edge within a chunk of eight.  X's padding and with it A's is zeros; Q's is zeros but for its
+// diagonal, where it is `a` throughout.  That the padding of Q X is zeros again is X's doing: a trace or a product of Q with itself would have those `a` in it.
 #pragma once
 #include "axo_common.hpp"
 #include "gemm_slim.hpp"
