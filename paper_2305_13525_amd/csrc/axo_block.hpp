@@ -360,6 +360,8 @@ constexpr double GATED_WIDE_MB[5] = {200.0, 200.0, 200.0, 200.0, 100.0};
 // The same for the tiles of gemm_tile.hpp: what their estimates have to be multiplied with for these products (small, wide, tall, mid, big; medians of the same
 // shapes), which read weights from memory and have longer epilogues.  Whatever is estimated quicker is taken: over those shapes the choice is 1.29 (forward), 1.63 and 1.99 times
 // quicker than these tiles throughout, 3 to 5 % slower than the best of all, and by more than 5 % slower than these tiles for two or three shapes in a hundred.
+// (The last row, of the product with a residual, is no such median: round numbers near the others', which were kept for the choice that they lead to.  Over 1200 drawn products of 1 to 400 tokens
+// and widths of 64 to 16384 that is 8 % slower than the best of all, in the geometric mean.)
 constexpr double GATED_TILES[5][5] = {{1.06, 1.66, 1.66, 1.21, 1.03}, {0.93, 1.37, 1.37, 1.41, 1.55}, {0.88, 1.47, 1.47, 1.21, 1.08}, {}, {1.0, 1.4, 1.4, 1.2, 1.05}};
 
 // How a product is cut into split-reduction tiles.
@@ -462,6 +464,7 @@ GatedPlan gated_plan(int Mo, int No, int R) {
     // 64 x 64 tiles that leave some CUs two and others one: a 64 x 128 tile for each CU is quicker, from four steps of a reduction on forward and from ten through the
     // activation's derivative, where G and U of a tile wait for its end.  Of 55 such shapes where 64 x 64 tiles were taken, forward 5 to 56 % over four steps (350 x 5928 x 1453 55 us
     // and 37, 1001 x 1027 x 515 12.1 and 10.1) and 0 to -5 % at two; backward 2 to 14 % from ten steps on (700 x 4000 x 1500 26.0 and 22.9), -10 to 3 % below.
+    // The product with a residual takes what goes for the forward pass, whose operands lie as its own do; it was not measured for this.
     if (OP != axo::GATED_DX && plan.tiles == Tiles::small && round_of_wide && small_tiles > NUM_CU && steps_in(R) >= (OP == axo::GATED_DACT ? 10 : 4)) plan.tiles = Tiles::wide;
     // Short reductions through the derivative are its reads of G and U and its stores, which go on beside each other where a CU has two tiles: 64 x 64 ones,
     // while there are few of them.  Of 126 shapes with reductions of 32 to 1024: for 128 x 128 tiles, to four steps and two a CU, 42 to 51 % quicker (2638 x 32 x 640 8.6 us and 6.0);
