@@ -48,6 +48,9 @@ SYMMETRIC = [((192, 192), "32 one whole", "32 one whole"), ((192, 2432), "32 non
              ((6976, 6976), "256 one shared", "256 one shared"), ((7488, 7488), "256 many whole", "256 many whole"), ((8000, 8000), "256 many slices", "256 many slices"),
              ((8000, 8256), "256 many own", "256 many slices"), ((9024, 9024), "256 many shared", "256 many shared")]
 
+# padded sizes s <= l whose product Q X, or X Q of a tall X, runs on 64 x 128 tiles: a round of them, more 64 x 64 ones
+OBLONG = [(1024, 1280), (1024, 1216), (1088, 1152)]
+
 
 def weights_of(s, l):
     """A wide and a tall weight, ragged, that are padded to these sizes."""

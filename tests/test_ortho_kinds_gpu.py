@@ -7,8 +7,8 @@ import ortho_plans as kinds
 import paper_2305_13525_amd as axo
 
 pytestmark = pytest.mark.gpu
-# every plan, and steps of one launch and of two
-WEIGHTS = [w for size, *_ in kinds.SYMMETRIC for w in kinds.weights_of(*size)] + [(51, 600), (600, 51), (115, 1000), (1000, 115), (50, 5000), (5000, 50), (120, 16000), (16000, 120)]
+# every plan, products on every kind of tile, and steps of one launch and of two
+WEIGHTS = [w for size in [size for size, *_ in kinds.SYMMETRIC] + kinds.OBLONG for w in kinds.weights_of(*size)] + [(51, 600), (600, 51), (115, 1000), (1000, 115), (50, 5000), (5000, 50), (120, 16000), (16000, 120)]
 
 
 def parity(v):
